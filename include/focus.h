@@ -313,6 +313,70 @@ focus_status focus_workspace_views(const focus_params *p, void *workspace,
                                    const int32_t **q_group_lists,
                                    const int32_t **k_group_lists);
 
+/* ---- positions and head norms in front of the attention ----
+ *
+ * Rotary positions: the first rot_dim components of a head are pairs (a, b); at position t pair i becomes
+ *     m (a cos - b sin, b cos + a sin),   angle = 2 pi t turns[i],
+ * with the magnitude m = 1 unless the scaling asks for another; the other components stay as they are.
+ * turns [rot_dim/2] fp64 is made once on the host by focus_rope_frequencies and handed over in DEVICE memory. */
+typedef enum { FOCUS_ROPE_HALF = 0,          /* pairs (i, i + rot_dim/2) */
+               FOCUS_ROPE_INTERLEAVED = 1    /* pairs (2i, 2i + 1)       */ } focus_rope_layout;
+
+/* How the frequencies w_i = base^(-2i/rot_dim) are scaled for contexts `factor` times the trained one:
+ *   NONE    as they are
+ *   LINEAR  w_i / factor (positions interpolated)
+ *   BASE    base * factor^(rot_dim/(rot_dim - 2)): the slowest pair is slowed by factor, the fastest not at all
+ *   PARTS   pairs that turn at least `fast` times in original_context keep w_i, those that turn at most `slow` times
+ *           take w_i / factor, a ramp over the pair index lies between; magnitude 0.1 ln(factor) + 1
+ *   BANDS   the same ends, the ramp linear in the number of turns; magnitude 1 */
+typedef enum { FOCUS_ROPE_NONE = 0, FOCUS_ROPE_LINEAR = 1, FOCUS_ROPE_BASE = 2, FOCUS_ROPE_PARTS = 3,
+               FOCUS_ROPE_BANDS = 4 } focus_rope_scaling;
+
+typedef struct {
+    int32_t rot_dim;           /* even, 2 .. 256                                            */
+    int32_t scaling;           /* focus_rope_scaling                                        */
+    double base;               /* > 1                                                       */
+    double factor;             /* >= 1 (not read with NONE)                                 */
+    double original_context;   /* > 0 (PARTS and BANDS)                                     */
+    double fast, slow;         /* fast > slow > 0 (PARTS and BANDS); 0 selects 32 and 1 with PARTS, 4 and 1 with BANDS */
+} focus_rope_spec;
+
+/* turns [rot_dim/2] (HOST): w_i / (2 pi); magnitude (HOST, nullable).  Pure host code, 64 bits. */
+focus_status focus_rope_frequencies(const focus_rope_spec *spec, double *turns, float *magnitude);
+
+typedef struct {
+    int32_t B, Hq, Hkv, n, d;  /* q [B,Hq,n,d], k [B,Hkv,n,d]; d in {64,80,96,128,256}; Hkv = 0: no k          */
+    int32_t rot_dim;           /* even, 0 .. d; 0 = no rotation (norms only)                                  */
+    int32_t layout;            /* focus_rope_layout                                                           */
+    int32_t dtype;             /* focus_dtype of q, k and everything of their shape                           */
+    float magnitude;           /* factor of the rotated components, 0 selects 1                               */
+    float eps;                 /* of the norms, >= 0                                                          */
+    /* strides as in focus_params: of q and k, and of their outputs (qo, ko) */
+    int64_t q_strides[3], k_strides[3], qo_strides[3], ko_strides[3];
+} focus_rope_params;
+
+/* q_out = rotated q, k_out = rotated k; inverse != 0 turns back (by the negative angle, times m: the gradient of the rotation).
+ * positions [B,n] int32 DEVICE, contiguous, any values; NULL: the index 0 .. n-1.  An output may be its input's
+ * memory if their strides are equal; otherwise outputs must not overlap inputs or each other.  One launch. */
+focus_status focus_rope(const focus_rope_params *rp, int32_t inverse, const void *q, const void *k,
+                        const int32_t *positions, const double *turns, void *q_out, void *k_out, void *stream);
+
+/* The same after a norm over the d components of every head: xh = x / sqrt(mean(x^2) + eps), times the gain
+ * q_weight / k_weight [d] fp32 DEVICE, then rotated; one rounding, at the end.  One launch. */
+focus_status focus_qk_norm_rope(const focus_rope_params *rp, const void *q, const void *k, const float *q_weight,
+                                const float *k_weight, const int32_t *positions, const double *turns, void *q_out,
+                                void *k_out, void *stream);
+
+/* Its gradient.  q, k: the inputs of the forward call; dq_out, dk_out: gradients of its outputs (strides qo, ko).
+ * Writes dq, dk (strides q, k; may be the memory of q, k or, with equal strides, of dq_out, dk_out) and the gains'
+ * gradients dq_weight, dk_weight [d] fp32, summed over all tokens and heads in a fixed order: the same bits every time.
+ * workspace: DEVICE scratch of focus_qk_norm_rope_workspace_size() bytes, 256-byte aligned.  Two launches. */
+focus_status focus_qk_norm_rope_workspace_size(const focus_rope_params *rp, size_t *bytes);
+focus_status focus_qk_norm_rope_bwd(const focus_rope_params *rp, const void *q, const void *k, const float *q_weight,
+                                    const float *k_weight, const int32_t *positions, const double *turns,
+                                    const void *dq_out, const void *dk_out, void *workspace, size_t workspace_bytes,
+                                    void *dq, void *dk, float *dq_weight, float *dk_weight, void *stream);
+
 /* Message of the last failure on this thread (static storage, never NULL). */
 const char *focus_last_error(void);
 

@@ -840,9 +840,183 @@ focus_status focus_workspace_views(const focus_params* p, void* workspace, const
     return FOCUS_OK;
 }
 
+namespace {
+
+// three strides in elements of a tensor [B,heads,n,d]: zeros mean contiguous; false if a row would not be 16-byte aligned
+bool take_strides(const int64_t* given, int heads, int n, int d, int elem, long long* out)
+{
+    if (given[0] == 0 && given[1] == 0 && given[2] == 0) {
+        out[0] = (long long)heads * n * d;
+        out[1] = (long long)n * d;
+        out[2] = d;
+        return true;
+    }
+    for (int i = 0; i < 3; ++i) {
+        out[i] = given[i];
+        if (given[i] < 0 || (given[i] * elem) % 16 != 0) return false;
+    }
+    return true;
+}
+
+bool same_strides(const long long* a, const long long* b) { return a[0] == b[0] && a[1] == b[1] && a[2] == b[2]; }
+
+focus_status check_shapes(int B, int Hq, int Hkv, int n, int d, int dtype)
+{
+    if (dtype != FOCUS_F32 && dtype != FOCUS_BF16 && dtype != FOCUS_F16) return fail(FOCUS_EINVAL, "unknown dtype %d", dtype);
+    if (d < 1) return fail(FOCUS_EINVAL, "d must be >= 1");
+    if (d != 64 && d != 80 && d != 96 && d != 128 && d != 256)
+        return fail(FOCUS_EUNSUPPORTED, "head dim %d is not built (64, 80, 96, 128 or 256)", d);
+    if (Hq > focus::MAX_HQ || Hkv > focus::MAX_HQ) return fail(FOCUS_EUNSUPPORTED, "more than %d heads is not built", focus::MAX_HQ);
+    if (n > (1 << 24)) return fail(FOCUS_EUNSUPPORTED, "n above 2^24 is not built");
+    if ((int64_t)B * Hq > 65535 || (int64_t)B * Hkv > 65535) return fail(FOCUS_EUNSUPPORTED, "B*H above 65535 is not built");
+    return FOCUS_OK;
+}
+
+focus_status make_rope_args(const focus_rope_params* rp, focus::RopeArgs* A)
+{
+    if (!rp) return fail(FOCUS_EINVAL, "rope params is NULL");
+    if (rp->B < 1 || rp->Hq < 1 || rp->Hkv < 0 || rp->n < 1)
+        return fail(FOCUS_EINVAL, "B, Hq, n must be >= 1 and Hkv >= 0 (got %d %d %d %d)", rp->B, rp->Hq, rp->n, rp->Hkv);
+    focus_status st = check_shapes(rp->B, rp->Hq, rp->Hkv, rp->n, rp->d, rp->dtype);
+    if (st != FOCUS_OK) return st;
+    if (rp->rot_dim < 0 || rp->rot_dim > rp->d || rp->rot_dim % 2 != 0)
+        return fail(FOCUS_EINVAL, "rot_dim must be even and in [0,d] (got %d)", rp->rot_dim);
+    if (rp->layout != FOCUS_ROPE_HALF && rp->layout != FOCUS_ROPE_INTERLEAVED) return fail(FOCUS_EINVAL, "unknown rope layout %d", rp->layout);
+    if (!std::isfinite(rp->magnitude)) return fail(FOCUS_EINVAL, "magnitude must be finite");
+    if (!(rp->eps >= 0.0f) || !std::isfinite(rp->eps)) return fail(FOCUS_EINVAL, "eps must be finite and >= 0");
+    memset(A, 0, sizeof(*A));
+    A->B = rp->B; A->Hq = rp->Hq; A->Hkv = rp->Hkv; A->n = rp->n; A->d = rp->d; A->rot = rp->rot_dim;
+    A->interleaved = rp->layout == FOCUS_ROPE_INTERLEAVED;
+    A->dtype = rp->dtype;
+    A->magnitude = rp->magnitude == 0.0f ? 1.0f : rp->magnitude;
+    A->eps = rp->eps;
+    const int elem = rp->dtype == FOCUS_F32 ? 4 : 2;
+    if (!take_strides(rp->q_strides, rp->Hq, rp->n, rp->d, elem, A->q.xs) || !take_strides(rp->qo_strides, rp->Hq, rp->n, rp->d, elem, A->q.ys) ||
+        !take_strides(rp->k_strides, rp->Hkv, rp->n, rp->d, elem, A->k.xs) || !take_strides(rp->ko_strides, rp->Hkv, rp->n, rp->d, elem, A->k.ys))
+        return fail(FOCUS_EINVAL, "strides must be >= 0 and multiples of 16 bytes");
+    return FOCUS_OK;
+}
+
+// pointers of the three rope calls; op as in launch_rope
+focus_status rope_call(const focus_rope_params* rp, int op, int inverse, const void* q, const void* k, const float* qw, const float* kw,
+                       const int32_t* positions, const double* turns, const void* gq, const void* gk, void* oq, void* ok,
+                       float* dqw, float* dkw, void* workspace, size_t bytes, void* stream, const char* who)
+{
+    focus::RopeArgs A;
+    focus_status st = make_rope_args(rp, &A);
+    if (st != FOCUS_OK) return st;
+    if (op == 0 && A.rot == 0) return fail(FOCUS_EINVAL, "rot_dim is 0: nothing to rotate");
+    const bool has_k = A.Hkv > 0;
+    if (!has_k && (k || kw || gk || ok || dkw)) return fail(FOCUS_EINVAL, "Hkv is 0: k and what belongs to it must be NULL");
+    if (!q || !oq || (has_k && (!k || !ok))) return fail(FOCUS_EINVAL, "inputs and outputs must not be NULL");
+    if (A.rot > 0 && !turns) return fail(FOCUS_EINVAL, "turns is NULL");
+    if (op != 0 && (!qw || (has_k && !kw))) return fail(FOCUS_EINVAL, "weights must not be NULL");
+    if (op == 2 && (!gq || !dqw || (has_k && (!gk || !dkw)))) return fail(FOCUS_EINVAL, "gradients must not be NULL");
+    if (misaligned16(q) || misaligned16(k) || misaligned16(gq) || misaligned16(gk) || misaligned16(oq) || misaligned16(ok))
+        return fail(FOCUS_EINVAL, "inputs and outputs must be 16-byte aligned");
+    if (((uintptr_t)qw | (uintptr_t)kw | (uintptr_t)dqw | (uintptr_t)dkw | (uintptr_t)positions) & 3 || (uintptr_t)turns & 7)
+        return fail(FOCUS_EINVAL, "weights and positions must be 4-byte aligned, turns 8-byte aligned");
+    if (oq == ok || oq == k || ok == q) return fail(FOCUS_EINVAL, "q's and k's tensors must not alias each other");
+    if (op != 2 && ((oq == q && !same_strides(A.q.xs, A.q.ys)) || (has_k && ok == k && !same_strides(A.k.xs, A.k.ys))))
+        return fail(FOCUS_EINVAL, "in place needs equal strides of input and output");
+    if (op == 2 && ((oq == gq && !same_strides(A.q.xs, A.q.ys)) || (has_k && ok == gk && !same_strides(A.k.xs, A.k.ys)) ||
+                    oq == gk || ok == gq || dqw == dkw))
+        return fail(FOCUS_EINVAL, "a gradient may share memory with its own input or, with equal strides, its own output's gradient only");
+    if (op == 2) {
+        if (!workspace) return fail(FOCUS_EINVAL, "workspace is NULL");
+        if (((uintptr_t)workspace & 255) != 0) return fail(FOCUS_EWORKSPACE, "workspace is not 256-byte aligned");
+        const size_t need = focus::rope_bwd_workspace(A);
+        if (bytes < need) return fail(FOCUS_EWORKSPACE, "workspace has %zu bytes, %zu needed", bytes, need);
+        A.partial = (float*)workspace;
+    }
+    A.invert = inverse != 0;
+    A.positions = positions;
+    A.turns = turns;
+    A.q.x = q; A.q.g = gq; A.q.w = qw; A.q.dw = dqw;
+    A.k.x = k; A.k.g = gk; A.k.w = kw; A.k.dw = dkw;
+    (op == 2 ? A.q.dx : A.q.y) = oq;
+    (op == 2 ? A.k.dx : A.k.y) = ok;
+    const hipError_t e = focus::launch_rope(A, op, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(FOCUS_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return FOCUS_OK;
+}
+
+}  // namespace
+
+focus_status focus_rope_frequencies(const focus_rope_spec* spec, double* turns, float* magnitude)
+{
+    if (!spec || !turns) return fail(FOCUS_EINVAL, "spec and turns must not be NULL");
+    const int r = spec->rot_dim;
+    if (r < 2 || r > 256 || r % 2 != 0) return fail(FOCUS_EINVAL, "rot_dim must be even and in [2,256] (got %d)", r);
+    if (spec->scaling < FOCUS_ROPE_NONE || spec->scaling > FOCUS_ROPE_BANDS) return fail(FOCUS_EINVAL, "unknown rope scaling %d", spec->scaling);
+    if (!(spec->base > 1.0) || !std::isfinite(spec->base)) return fail(FOCUS_EINVAL, "base must be finite and > 1");
+    const double f = spec->scaling == FOCUS_ROPE_NONE ? 1.0 : spec->factor;
+    if (!(f >= 1.0) || !std::isfinite(f)) return fail(FOCUS_EINVAL, "factor must be finite and >= 1");
+    const bool ramp = spec->scaling == FOCUS_ROPE_PARTS || spec->scaling == FOCUS_ROPE_BANDS;
+    const double fast = spec->fast == 0.0 ? (spec->scaling == FOCUS_ROPE_PARTS ? 32.0 : 4.0) : spec->fast;
+    const double slow = spec->slow == 0.0 ? 1.0 : spec->slow;
+    if (ramp && (!(spec->original_context > 0.0) || !std::isfinite(spec->original_context)))
+        return fail(FOCUS_EINVAL, "original_context must be finite and > 0");
+    if (ramp && (!(slow > 0.0) || !(fast > slow) || !std::isfinite(fast))) return fail(FOCUS_EINVAL, "fast > slow > 0 is needed");
+    if (spec->scaling == FOCUS_ROPE_BASE && r == 2) return fail(FOCUS_EINVAL, "scaling the base needs rot_dim > 2");
+    const double two_pi = 6.283185307179586476925;
+    const double base = spec->scaling == FOCUS_ROPE_BASE ? spec->base * std::pow(f, r / (r - 2.0)) : spec->base;
+    // pair index at which a frequency turns `count` times in the original context
+    auto pair_of = [&](double count) { return r * std::log(spec->original_context / (count * two_pi)) / (2.0 * std::log(base)); };
+    double lo = 0.0, hi = 0.0;
+    if (spec->scaling == FOCUS_ROPE_PARTS) {
+        lo = std::max(std::floor(pair_of(fast)), 0.0);
+        hi = std::min(std::ceil(pair_of(slow)), r - 1.0);
+    }
+    for (int i = 0; i < r / 2; ++i) {
+        double w = std::pow(base, -2.0 * i / r);
+        double slowed = 0.0;                               // share of w / factor
+        if (spec->scaling == FOCUS_ROPE_LINEAR) slowed = 1.0;
+        else if (spec->scaling == FOCUS_ROPE_PARTS) slowed = std::min(1.0, std::max(0.0, (i - lo) / std::max(hi - lo, 0.001)));
+        else if (spec->scaling == FOCUS_ROPE_BANDS)
+            slowed = 1.0 - std::min(1.0, std::max(0.0, (spec->original_context * w / two_pi - slow) / (fast - slow)));
+        turns[i] = (w * (1.0 - slowed) + w / f * slowed) / two_pi;
+    }
+    if (magnitude) *magnitude = spec->scaling == FOCUS_ROPE_PARTS ? (float)(0.1 * std::log(f) + 1.0) : 1.0f;
+    return FOCUS_OK;
+}
+
+focus_status focus_rope(const focus_rope_params* rp, int32_t inverse, const void* q, const void* k, const int32_t* positions,
+                        const double* turns, void* q_out, void* k_out, void* stream)
+{
+    return rope_call(rp, 0, inverse, q, k, nullptr, nullptr, positions, turns, nullptr, nullptr, q_out, k_out, nullptr, nullptr,
+                     nullptr, 0, stream, "focus_rope");
+}
+
+focus_status focus_qk_norm_rope(const focus_rope_params* rp, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                                const int32_t* positions, const double* turns, void* q_out, void* k_out, void* stream)
+{
+    return rope_call(rp, 1, 0, q, k, q_weight, k_weight, positions, turns, nullptr, nullptr, q_out, k_out, nullptr, nullptr,
+                     nullptr, 0, stream, "focus_qk_norm_rope");
+}
+
+focus_status focus_qk_norm_rope_workspace_size(const focus_rope_params* rp, size_t* bytes)
+{
+    if (!bytes) return fail(FOCUS_EINVAL, "bytes is NULL");
+    focus::RopeArgs A;
+    focus_status st = make_rope_args(rp, &A);
+    if (st != FOCUS_OK) return st;
+    *bytes = align256(focus::rope_bwd_workspace(A));
+    return FOCUS_OK;
+}
+
+focus_status focus_qk_norm_rope_bwd(const focus_rope_params* rp, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                                    const int32_t* positions, const double* turns, const void* dq_out, const void* dk_out,
+                                    void* workspace, size_t workspace_bytes, void* dq, void* dk, float* dq_weight, float* dk_weight,
+                                    void* stream)
+{
+    return rope_call(rp, 2, 0, q, k, q_weight, k_weight, positions, turns, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace,
+                     workspace_bytes, stream, "focus_qk_norm_rope_bwd");
+}
+
 const char* focus_last_error(void) { return g_err; }
 
-int focus_version(void) { return 100; }
+int focus_version(void) { return 200; }
 
 #ifndef FOCUS_BUILD_ID
 #define FOCUS_BUILD_ID "unknown"

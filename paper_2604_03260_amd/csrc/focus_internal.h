@@ -267,4 +267,27 @@ hipError_t launch_attn_mfma(const Layout& L, const HeadMap& hm, const void* q, c
                             const void* v, const float* g, char* ws, void* out, float* lse, int32_t* row_pairs,
                             hipStream_t st);
 
+// Rotation, head norms with rotation, and their gradient (focus_rope.hip): q's side and k's side of one call.
+struct RopeSide {
+    const void* x;             // input
+    void* y;                   // output (rotation, norm and rotation)
+    const void* g;             // gradient of the output
+    void* dx;                  // gradient of the input
+    const float* w;            // [d] gain of the norm
+    float* dw;                 // [d] its gradient
+    long long xs[3], ys[3];    // strides of x and dx, of y and g, in elements (batch, head, position)
+};
+struct RopeArgs {
+    RopeSide q, k;
+    int B, Hq, Hkv, n, d, rot;
+    int interleaved, dtype, invert;
+    int heads;                 // heads of a work-group's walk (set by the launch)
+    float magnitude, eps;
+    const int* positions;      // [B,n] or null: the index
+    const double* turns;       // [rot/2]
+    float* partial;            // partial sums of dw (gradient)
+};
+size_t rope_bwd_workspace(const RopeArgs& A);
+hipError_t launch_rope(const RopeArgs& A, int op, hipStream_t st);     // op: 0 rotation, 1 norm and rotation, 2 the gradient of 1
+
 }  // namespace focus

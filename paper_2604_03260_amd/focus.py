@@ -28,6 +28,8 @@ EXPORTS = ("focus_workspace_size", "focus_assign", "focus_attn_fwd", "focus_work
            "focus_decode_prefill_tokens", "focus_decode_step_tokens",
            "focus_soft_workspace_size", "focus_attn_soft_fwd",
            "focus_attn_fwd_vector", "focus_attn_soft_fwd_vector",
+           "focus_rope_frequencies", "focus_rope", "focus_qk_norm_rope",
+           "focus_qk_norm_rope_workspace_size", "focus_qk_norm_rope_bwd",
            "focus_last_error", "focus_version", "focus_build_id")
 
 
@@ -48,6 +50,23 @@ class FocusParams(ctypes.Structure):
         ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
         ("head_map", ctypes.POINTER(ctypes.c_int32)),
         ("q_strides", ctypes.c_int64 * 3), ("kv_strides", ctypes.c_int64 * 3), ("o_strides", ctypes.c_int64 * 3),
+    ]
+
+
+class FocusRopeSpec(ctypes.Structure):
+    _fields_ = [
+        ("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+        ("original_context", ctypes.c_double), ("fast", ctypes.c_double), ("slow", ctypes.c_double),
+    ]
+
+
+class FocusRopeParams(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("n", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("magnitude", ctypes.c_float), ("eps", ctypes.c_float),
+        ("q_strides", ctypes.c_int64 * 3), ("k_strides", ctypes.c_int64 * 3),
+        ("qo_strides", ctypes.c_int64 * 3), ("ko_strides", ctypes.c_int64 * 3),
     ]
 
 
@@ -131,6 +150,17 @@ def load_library():
     lib.focus_route_noalloc.restype = ctypes.c_int
     lib.focus_assign_tokens.argtypes = [pp, vp, vp, vp, sz, vp, vp]
     lib.focus_assign_tokens.restype = ctypes.c_int
+    op = ctypes.POINTER(FocusRopeParams)
+    lib.focus_rope_frequencies.argtypes = [ctypes.POINTER(FocusRopeSpec), vp, ctypes.POINTER(ctypes.c_float)]
+    lib.focus_rope_frequencies.restype = ctypes.c_int
+    lib.focus_rope.argtypes = [op, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp]
+    lib.focus_rope.restype = ctypes.c_int
+    lib.focus_qk_norm_rope.argtypes = [op, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.focus_qk_norm_rope.restype = ctypes.c_int
+    lib.focus_qk_norm_rope_workspace_size.argtypes = [op, ctypes.POINTER(sz)]
+    lib.focus_qk_norm_rope_workspace_size.restype = ctypes.c_int
+    lib.focus_qk_norm_rope_bwd.argtypes = [op] + [vp] * 9 + [sz] + [vp] * 5
+    lib.focus_qk_norm_rope_bwd.restype = ctypes.c_int
     lib.focus_last_error.argtypes = []
     lib.focus_last_error.restype = ctypes.c_char_p
     lib.focus_version.argtypes = []
@@ -367,3 +397,64 @@ def focus_workspace_views(p, workspace):
 def alloc_workspace(p, device="cuda"):
     nbytes = focus_workspace_size(p)
     return torch.empty(((nbytes + 255) // 256) * 256, dtype=torch.uint8, device=device)
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
+
+
+def focus_rope_frequencies(rot_dim, base=10000.0, scaling="none", factor=1.0, original_context=0.0, fast=0.0, slow=0.0):
+    """(turns [rot_dim/2] float64 on the host, magnitude): turns go to the device once, magnitude into make_rope_params."""
+    spec = FocusRopeSpec(rot_dim, ROPE_SCALINGS[scaling], base, factor, original_context, fast, slow)
+    turns = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64)
+    magnitude = ctypes.c_float(1.0)
+    _check(load_library().focus_rope_frequencies(ctypes.byref(spec), _ptr(turns), ctypes.byref(magnitude)))
+    return turns, magnitude.value
+
+
+def make_rope_params(B, Hq, Hkv, n, d, rot_dim, layout="half", dtype="bf16", magnitude=1.0, eps=1e-6, q_strides=None,
+                     k_strides=None, qo_strides=None, ko_strides=None):
+    """Strides: None = contiguous [B,H,n,d]; Hkv = 0: queries only."""
+    arr = lambda st: (ctypes.c_int64 * 3)(*(st if st is not None else (0, 0, 0)))
+    return FocusRopeParams(B, Hq, Hkv, n, d, rot_dim, ROPE_LAYOUTS[layout], DTYPES[dtype], magnitude, eps, arr(q_strides),
+                           arr(k_strides), arr(qo_strides), arr(ko_strides))
+
+
+def _check_rope(rp, positions, turns, *weights):
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous()
+                                 and positions.numel() == rp.B * rp.n)
+    assert turns is None or (turns.dtype == torch.float64 and turns.is_contiguous() and turns.numel() * 2 >= rp.rot_dim)
+    for w in weights:
+        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == rp.d)
+
+
+def focus_rope(rp, q, k, positions, turns, q_out, k_out, inverse=False):
+    """q, k turned by their positions (int32 [B,n] on the device, None: the index); inverse: turned back."""
+    _check_rope(rp, positions, turns)
+    _check(load_library().focus_rope(ctypes.byref(rp), 1 if inverse else 0, _ptr(q), _ptr(k), _ptr(positions), _ptr(turns),
+                                     _ptr(q_out), _ptr(k_out), _stream()))
+
+
+def focus_qk_norm_rope(rp, q, k, q_weight, k_weight, positions, turns, q_out, k_out):
+    _check_rope(rp, positions, turns, q_weight, k_weight)
+    _check(load_library().focus_qk_norm_rope(ctypes.byref(rp), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight),
+                                             _ptr(positions), _ptr(turns), _ptr(q_out), _ptr(k_out), _stream()))
+
+
+def focus_qk_norm_rope_workspace_size(rp):
+    out = ctypes.c_size_t(0)
+    _check(load_library().focus_qk_norm_rope_workspace_size(ctypes.byref(rp), ctypes.byref(out)))
+    return out.value
+
+
+def alloc_qk_norm_rope_workspace(rp, device="cuda"):
+    return torch.empty(max(focus_qk_norm_rope_workspace_size(rp), 256), dtype=torch.uint8, device=device)
+
+
+def focus_qk_norm_rope_bwd(rp, q, k, q_weight, k_weight, positions, turns, dq_out, dk_out, workspace, dq, dk, dq_weight,
+                           dk_weight):
+    _check_rope(rp, positions, turns, q_weight, k_weight, dq_weight, dk_weight)
+    _check(load_library().focus_qk_norm_rope_bwd(
+        ctypes.byref(rp), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(positions), _ptr(turns), _ptr(dq_out),
+        _ptr(dk_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(dq), _ptr(dk), _ptr(dq_weight),
+        _ptr(dk_weight), _stream()))
