@@ -377,6 +377,60 @@ focus_status focus_qk_norm_rope_bwd(const focus_rope_params *rp, const void *q, 
                                     const void *dq_out, const void *dk_out, void *workspace, size_t workspace_bytes,
                                     void *dq, void *dk, float *dq_weight, float *dk_weight, void *stream);
 
+/* ---- attention of a sliding window with sinks: the local layers between Focus layers ----
+ *
+ * Row i sees key j iff j <= i and (i - j < window or j < sinks): the window of focus_params without groups, and the first
+ * `sinks` tokens for every row.  logit = scale q.k, soft-capped before the mask if softcap > 0; exact softmax.  Every row
+ * sees itself, so no row is empty.  Tokens that a row does not see have no influence on it, whatever their values. */
+typedef struct {
+    int32_t B, Hq, Hkv, n, d;  /* as in focus_params; Hq % Hkv == 0, head h reads KV head h / (Hq / Hkv)      */
+    int32_t window;            /* >= 1                                                                        */
+    int32_t sinks;             /* >= 0                                                                        */
+    int32_t dtype;             /* focus_dtype of every tensor of rows                                         */
+    int32_t packed;            /* 1: the B sequences lie in ONE [1,H,n,d] set of tensors, where spans says; the
+                                  batch strides are not read and lse is [Hq,n]                                */
+    int32_t span_max;          /* longest span (0 selects n); a longer one is cut to it                       */
+    float scale;               /* 0 selects 1/sqrt(d)                                                         */
+    float softcap;             /* 0 = off                                                                     */
+    int64_t q_strides[3], kv_strides[3], o_strides[3];   /* as in focus_params; dq has q's, dk and dv have kv's, dout has out's */
+} focus_window_params;
+
+/* spans [B,2] int32 DEVICE, nullable unless packed: sequence b is the rows first .. first + length - 1 (cut to the n rows), its positions count
+ * from first, and so do its sinks.  Length 0 is allowed; a negative first or length, or first >= n, is no rows.  Rows in no span are neither read nor written, in any output.
+ * Spans of one packed call must not overlap.
+ * out as q; lse (nullable) [B,Hq,n] fp32 natural log.  One launch, no workspace. */
+focus_status focus_window_attn_fwd(const focus_window_params *p, const void *q, const void *k, const void *v,
+                                   const int32_t *spans, void *out, float *lse, void *stream);
+
+/* Gradients of q, k, v from dout, with the forward call's out and lse.  Sums over rows and over the query heads of a KV
+ * head are taken in a fixed order: the same bits every time.  workspace: DEVICE scratch of
+ * focus_window_bwd_workspace_size() bytes, 256-byte aligned.  dq, dk, dv must not overlap anything else. */
+focus_status focus_window_bwd_workspace_size(const focus_window_params *p, size_t *bytes);
+focus_status focus_window_attn_bwd(const focus_window_params *p, const void *q, const void *k, const void *v,
+                                   const void *out, const float *lse, const void *dout, const int32_t *spans,
+                                   void *workspace, size_t workspace_bytes, void *dq, void *dk, void *dv, void *stream);
+
+/* Generation over caches k_cache, v_cache [B,Hkv,capacity,d] (contiguous, 16-byte aligned) that may be shorter than the
+ * sequence: position t lies in row t while t < capacity, else in row sinks + (t - sinks) mod (capacity - sinks), so the sinks
+ * stay and the rest goes round.  Positions at or past the capacity need capacity - sinks >= window.
+ *
+ * focus_window_cache_fill copies what a prompt leaves in the caches: k, v (strides kv, spans as above; p->n is
+ * the prompt's) to the rows of their positions.  Rows of positions that do not exist stay as they are.
+ * FOCUS_EINVAL if span_max exceeds the capacity and the caches cannot go round. */
+focus_status focus_window_cache_fill(const focus_window_params *p, int32_t capacity, const void *k, const void *v,
+                                     const int32_t *spans, void *k_cache, void *v_cache, void *stream);
+
+/* One token for each sequence, at position pos_dev[b] (int32 DEVICE [B], read when the kernels run: one captured graph
+ * serves a generation loop).  p->n is the CAPACITY; the strides must be 0 and packed 0.  Stores k_new, v_new [B,Hkv,d] in the
+ * row of their position, then q_new [B,Hq,d] attends.  A sequence whose position is negative, or at or past the capacity of
+ * caches that cannot go round, is skipped: caches and outputs stay untouched.  out [B,Hq,d], lse (nullable) [B,Hq]
+ * fp32.  workspace: DEVICE scratch of focus_window_decode_workspace_size() bytes, 256-byte aligned; calls that share one
+ * must not overlap. */
+focus_status focus_window_decode_workspace_size(const focus_window_params *p, size_t *bytes);
+focus_status focus_window_decode_step_at(const focus_window_params *p, const int32_t *pos_dev, const void *q_new,
+                                         const void *k_new, const void *v_new, void *k_cache, void *v_cache,
+                                         void *workspace, size_t workspace_bytes, void *out, float *lse, void *stream);
+
 /* Message of the last failure on this thread (static storage, never NULL). */
 const char *focus_last_error(void);
 

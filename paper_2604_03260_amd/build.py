@@ -8,7 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfocus.so")
 SOURCES = ["focus_api.hip", "focus_assign.hip", "focus_attn_simple.hip", "focus_attn_f32.hip", "focus_attn_short.hip", "focus_attn_mfma.hip",
-           "focus_route.hip", "focus_decode.hip", "focus_rope.hip"]
+           "focus_route.hip", "focus_decode.hip", "focus_rope.hip",
+           "focus_window.hip", "focus_window_bwd.hip", "focus_window_decode.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=on", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-result", "-Wno-unused-command-line-argument"]

@@ -1014,6 +1014,186 @@ focus_status focus_qk_norm_rope_bwd(const focus_rope_params* rp, const void* q, 
                      workspace_bytes, stream, "focus_qk_norm_rope_bwd");
 }
 
+namespace {
+
+focus_status make_window_args(const focus_window_params* p, focus::WindowArgs* A)
+{
+    if (!p) return fail(FOCUS_EINVAL, "window params is NULL");
+    if (p->B < 1 || p->Hq < 1 || p->Hkv < 1 || p->n < 1)
+        return fail(FOCUS_EINVAL, "B, Hq, Hkv, n must be >= 1 (got %d %d %d %d)", p->B, p->Hq, p->Hkv, p->n);
+    focus_status st = check_shapes(p->B, p->Hq, p->Hkv, p->n, p->d, p->dtype);
+    if (st != FOCUS_OK) return st;
+    if (p->Hq % p->Hkv != 0) return fail(FOCUS_EINVAL, "Hq (%d) is not a multiple of Hkv (%d)", p->Hq, p->Hkv);
+    if (p->window < 1) return fail(FOCUS_EINVAL, "window must be >= 1 (got %d)", p->window);
+    if (p->sinks < 0) return fail(FOCUS_EINVAL, "sinks must be >= 0 (got %d)", p->sinks);
+    if (p->packed != 0 && p->packed != 1) return fail(FOCUS_EINVAL, "packed must be 0 or 1");
+    if (p->span_max < 0 || p->span_max > p->n) return fail(FOCUS_EINVAL, "span_max must be in [0,n] (got %d)", p->span_max);
+    if (!(p->scale >= 0.0f) || !std::isfinite(p->scale)) return fail(FOCUS_EINVAL, "scale must be finite and >= 0");
+    if (!(p->softcap >= 0.0f) || !std::isfinite(p->softcap)) return fail(FOCUS_EINVAL, "softcap must be finite and >= 0");
+    memset(A, 0, sizeof(*A));
+    A->B = p->B; A->Hq = p->Hq; A->Hkv = p->Hkv; A->n = p->n; A->d = p->d;
+    A->window = std::min(p->window, p->n);
+    A->sinks = std::min(p->sinks, p->n);
+    A->dtype = p->dtype; A->packed = p->packed;
+    A->span_max = p->span_max ? p->span_max : p->n;
+    A->scale = (p->scale > 0.0f) ? p->scale : (float)(1.0 / std::sqrt((double)p->d));
+    A->softcap = p->softcap;
+    const int elem = p->dtype == FOCUS_F32 ? 4 : 2;
+    if (!take_strides(p->q_strides, p->Hq, p->n, p->d, elem, A->qs) || !take_strides(p->kv_strides, p->Hkv, p->n, p->d, elem, A->ks) ||
+        !take_strides(p->o_strides, p->Hq, p->n, p->d, elem, A->os))
+        return fail(FOCUS_EINVAL, "strides must be >= 0 and multiples of 16 bytes");
+    return FOCUS_OK;
+}
+
+focus_status check_spans(const focus::WindowArgs& A, const int32_t* spans)
+{
+    if (A.packed && !spans) return fail(FOCUS_EINVAL, "packed sequences need spans");
+    if (((uintptr_t)spans & 7) != 0) return fail(FOCUS_EINVAL, "spans must be 8-byte aligned");
+    return FOCUS_OK;
+}
+
+focus_status check_scratch(const void* ws, size_t bytes, size_t need)
+{
+    if (!ws) return fail(FOCUS_EINVAL, "workspace is NULL");
+    if (((uintptr_t)ws & 255) != 0) return fail(FOCUS_EWORKSPACE, "workspace is not 256-byte aligned");
+    if (bytes < need) return fail(FOCUS_EWORKSPACE, "workspace has %zu bytes, %zu needed", bytes, need);
+    return FOCUS_OK;
+}
+
+bool all_strides_zero(const focus_window_params* p)
+{
+    for (int i = 0; i < 3; ++i)
+        if (p->q_strides[i] != 0 || p->kv_strides[i] != 0 || p->o_strides[i] != 0) return false;
+    return true;
+}
+
+// the caches of a generation call: window and sinks as given, not cut to the capacity
+focus_status make_cache_args(const focus_window_params* p, focus::WindowArgs* A)
+{
+    focus_status st = make_window_args(p, A);
+    if (st != FOCUS_OK) return st;
+    if (p->packed || !all_strides_zero(p)) return fail(FOCUS_EUNSUPPORTED, "the caches are contiguous: strides must be 0 and packed 0");
+    A->window = p->window;
+    A->sinks = p->sinks;
+    return FOCUS_OK;
+}
+
+}  // namespace
+
+focus_status focus_window_attn_fwd(const focus_window_params* p, const void* q, const void* k, const void* v, const int32_t* spans,
+                                   void* out, float* lse, void* stream)
+{
+    focus::WindowArgs A;
+    focus_status st = make_window_args(p, &A);
+    if (st == FOCUS_OK) st = check_spans(A, spans);
+    if (st != FOCUS_OK) return st;
+    if (!q || !k || !v || !out) return fail(FOCUS_EINVAL, "q, k, v and out must not be NULL");
+    if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(out))
+        return fail(FOCUS_EINVAL, "q, k, v and out must be 16-byte aligned");
+    if (out == q || out == k || out == v) return fail(FOCUS_EINVAL, "out must not alias an input");
+    if (((uintptr_t)lse & 3) != 0) return fail(FOCUS_EINVAL, "lse must be 4-byte aligned");
+    A.spans = (const int2*)spans;
+    const hipError_t e = focus::launch_window_fwd(A, q, k, v, out, lse, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(FOCUS_EHIP, "focus_window_attn_fwd: %s", hipGetErrorString(e));
+    return FOCUS_OK;
+}
+
+focus_status focus_window_bwd_workspace_size(const focus_window_params* p, size_t* bytes)
+{
+    if (!bytes) return fail(FOCUS_EINVAL, "bytes is NULL");
+    focus::WindowArgs A;
+    focus_status st = make_window_args(p, &A);
+    if (st != FOCUS_OK) return st;
+    *bytes = align256(focus::window_bwd_workspace(A));
+    return FOCUS_OK;
+}
+
+focus_status focus_window_attn_bwd(const focus_window_params* p, const void* q, const void* k, const void* v, const void* out,
+                                   const float* lse, const void* dout, const int32_t* spans, void* workspace, size_t workspace_bytes,
+                                   void* dq, void* dk, void* dv, void* stream)
+{
+    focus::WindowArgs A;
+    focus_status st = make_window_args(p, &A);
+    if (st == FOCUS_OK) st = check_spans(A, spans);
+    if (st != FOCUS_OK) return st;
+    const void* in[] = {q, k, v, out, dout};
+    void* res[] = {dq, dk, dv};
+    for (const void* x : in)
+        if (!x) return fail(FOCUS_EINVAL, "q, k, v, out and dout must not be NULL");
+    for (int i = 0; i < 3; ++i) {
+        if (!res[i]) return fail(FOCUS_EINVAL, "dq, dk and dv must not be NULL");
+        if (misaligned16(res[i])) return fail(FOCUS_EINVAL, "dq, dk and dv must be 16-byte aligned");
+        for (const void* x : in)
+            if (res[i] == x) return fail(FOCUS_EINVAL, "dq, dk and dv must not alias an input");
+        if (res[i] == res[(i + 1) % 3]) return fail(FOCUS_EINVAL, "dq, dk and dv must not alias each other");
+    }
+    for (const void* x : in)
+        if (misaligned16(x)) return fail(FOCUS_EINVAL, "q, k, v, out and dout must be 16-byte aligned");
+    if (!lse || ((uintptr_t)lse & 3) != 0) return fail(FOCUS_EINVAL, "lse must be there, 4-byte aligned");
+    st = check_scratch(workspace, workspace_bytes, focus::window_bwd_workspace(A));
+    if (st != FOCUS_OK) return st;
+    A.spans = (const int2*)spans;
+    const hipError_t e = focus::launch_window_bwd(A, q, k, v, out, lse, dout, (char*)workspace, dq, dk, dv, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(FOCUS_EHIP, "focus_window_attn_bwd: %s", hipGetErrorString(e));
+    return FOCUS_OK;
+}
+
+focus_status focus_window_cache_fill(const focus_window_params* p, int32_t capacity, const void* k, const void* v, const int32_t* spans,
+                                     void* k_cache, void* v_cache, void* stream)
+{
+    focus::WindowArgs A;
+    focus_status st = make_window_args(p, &A);
+    if (st == FOCUS_OK) st = check_spans(A, spans);
+    if (st != FOCUS_OK) return st;
+    A.window = p->window;
+    A.sinks = p->sinks;
+    if (capacity < 1) return fail(FOCUS_EINVAL, "capacity must be >= 1 (got %d)", capacity);
+    if (capacity > (1 << 24)) return fail(FOCUS_EUNSUPPORTED, "a capacity above 2^24 is not built");
+    if (A.span_max > capacity && (int64_t)capacity - A.sinks < A.window)
+        return fail(FOCUS_EINVAL, "%d tokens do not fit caches of %d rows that cannot go round (capacity - sinks >= window)", A.span_max, capacity);
+    if (!k || !v || !k_cache || !v_cache) return fail(FOCUS_EINVAL, "k, v and the caches must not be NULL");
+    if (misaligned16(k) || misaligned16(v) || misaligned16(k_cache) || misaligned16(v_cache))
+        return fail(FOCUS_EINVAL, "k, v and the caches must be 16-byte aligned");
+    if (k_cache == k || k_cache == v || v_cache == k || v_cache == v || k_cache == v_cache)
+        return fail(FOCUS_EINVAL, "the caches must not alias k, v or each other");
+    A.spans = (const int2*)spans;
+    const hipError_t e = focus::launch_window_fill(A, capacity, k, v, k_cache, v_cache, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(FOCUS_EHIP, "focus_window_cache_fill: %s", hipGetErrorString(e));
+    return FOCUS_OK;
+}
+
+focus_status focus_window_decode_workspace_size(const focus_window_params* p, size_t* bytes)
+{
+    if (!bytes) return fail(FOCUS_EINVAL, "bytes is NULL");
+    focus::WindowArgs A;
+    focus_status st = make_cache_args(p, &A);
+    if (st != FOCUS_OK) return st;
+    *bytes = align256(std::max<size_t>(focus::window_decode_workspace(A), 1));
+    return FOCUS_OK;
+}
+
+focus_status focus_window_decode_step_at(const focus_window_params* p, const int32_t* pos_dev, const void* q_new, const void* k_new,
+                                         const void* v_new, void* k_cache, void* v_cache, void* workspace, size_t workspace_bytes,
+                                         void* out, float* lse, void* stream)
+{
+    focus::WindowArgs A;
+    focus_status st = make_cache_args(p, &A);
+    if (st != FOCUS_OK) return st;
+    if (!pos_dev || !q_new || !k_new || !v_new || !k_cache || !v_cache || !out)
+        return fail(FOCUS_EINVAL, "positions, q, k, v, the caches and out must not be NULL");
+    if (misaligned16(q_new) || misaligned16(k_new) || misaligned16(v_new) || misaligned16(k_cache) || misaligned16(v_cache) || misaligned16(out))
+        return fail(FOCUS_EINVAL, "q, k, v, the caches and out must be 16-byte aligned");
+    if (((uintptr_t)pos_dev & 3) != 0 || ((uintptr_t)lse & 3) != 0) return fail(FOCUS_EINVAL, "pos_dev and lse must be 4-byte aligned");
+    if (out == q_new || out == k_new || out == v_new || out == k_cache || out == v_cache || k_cache == v_cache)
+        return fail(FOCUS_EINVAL, "out and the caches must not alias each other or an input");
+    st = check_scratch(workspace, workspace_bytes, focus::window_decode_workspace(A));
+    if (st != FOCUS_OK) return st;
+    const hipError_t e = focus::launch_window_decode(A, pos_dev, q_new, k_new, v_new, k_cache, v_cache, (char*)workspace, out, lse,
+                                                     (hipStream_t)stream);
+    if (e != hipSuccess) return fail(FOCUS_EHIP, "focus_window_decode_step_at: %s", hipGetErrorString(e));
+    return FOCUS_OK;
+}
+
 const char* focus_last_error(void) { return g_err; }
 
 int focus_version(void) { return 200; }

@@ -290,4 +290,23 @@ struct RopeArgs {
 size_t rope_bwd_workspace(const RopeArgs& A);
 hipError_t launch_rope(const RopeArgs& A, int op, hipStream_t st);     // op: 0 rotation, 1 norm and rotation, 2 the gradient of 1
 
+// Sliding window with sinks (focus_window*.hip).
+struct WindowArgs {
+    int B, Hq, Hkv, n, d;
+    int window, sinks;         // both at most n (prefill, training)
+    int dtype, packed, span_max;
+    float scale, softcap;
+    long long qs[3], ks[3], os[3];     // strides of q and dq, of k, v, dk and dv, of out and dout (batch 0 if packed)
+    const int2* spans;         // [B] (first row, length) or null
+};
+hipError_t launch_window_fwd(const WindowArgs& A, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st);
+size_t window_bwd_workspace(const WindowArgs& A);
+hipError_t launch_window_bwd(const WindowArgs& A, const void* q, const void* k, const void* v, const void* out, const float* lse,
+                             const void* dout, char* ws, void* dq, void* dk, void* dv, hipStream_t st);
+hipError_t launch_window_fill(const WindowArgs& A, int capacity, const void* k, const void* v, void* kc, void* vc, hipStream_t st);
+size_t window_decode_workspace(const WindowArgs& A);
+hipError_t launch_window_decode(const WindowArgs& A, const int* pos, const void* q, const void* kn, const void* vn, void* kc, void* vc,
+                                char* ws, void* out, float* lse, hipStream_t st);
+
+
 }  // namespace focus

@@ -30,6 +30,8 @@ EXPORTS = ("focus_workspace_size", "focus_assign", "focus_attn_fwd", "focus_work
            "focus_attn_fwd_vector", "focus_attn_soft_fwd_vector",
            "focus_rope_frequencies", "focus_rope", "focus_qk_norm_rope",
            "focus_qk_norm_rope_workspace_size", "focus_qk_norm_rope_bwd",
+           "focus_window_attn_fwd", "focus_window_bwd_workspace_size", "focus_window_attn_bwd",
+           "focus_window_cache_fill", "focus_window_decode_workspace_size", "focus_window_decode_step_at",
            "focus_last_error", "focus_version", "focus_build_id")
 
 
@@ -67,6 +69,15 @@ class FocusRopeParams(ctypes.Structure):
         ("magnitude", ctypes.c_float), ("eps", ctypes.c_float),
         ("q_strides", ctypes.c_int64 * 3), ("k_strides", ctypes.c_int64 * 3),
         ("qo_strides", ctypes.c_int64 * 3), ("ko_strides", ctypes.c_int64 * 3),
+    ]
+
+
+class FocusWindowParams(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("n", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("dtype", ctypes.c_int32), ("packed", ctypes.c_int32),
+        ("span_max", ctypes.c_int32), ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+        ("q_strides", ctypes.c_int64 * 3), ("kv_strides", ctypes.c_int64 * 3), ("o_strides", ctypes.c_int64 * 3),
     ]
 
 
@@ -161,6 +172,18 @@ def load_library():
     lib.focus_qk_norm_rope_workspace_size.restype = ctypes.c_int
     lib.focus_qk_norm_rope_bwd.argtypes = [op] + [vp] * 9 + [sz] + [vp] * 5
     lib.focus_qk_norm_rope_bwd.restype = ctypes.c_int
+    wp = ctypes.POINTER(FocusWindowParams)
+    lib.focus_window_attn_fwd.argtypes = [wp] + [vp] * 7
+    lib.focus_window_attn_fwd.restype = ctypes.c_int
+    for fn in (lib.focus_window_bwd_workspace_size, lib.focus_window_decode_workspace_size):
+        fn.argtypes = [wp, ctypes.POINTER(sz)]
+        fn.restype = ctypes.c_int
+    lib.focus_window_attn_bwd.argtypes = [wp] + [vp] * 8 + [sz] + [vp] * 4
+    lib.focus_window_attn_bwd.restype = ctypes.c_int
+    lib.focus_window_cache_fill.argtypes = [wp, ctypes.c_int32] + [vp] * 6
+    lib.focus_window_cache_fill.restype = ctypes.c_int
+    lib.focus_window_decode_step_at.argtypes = [wp] + [vp] * 7 + [sz] + [vp] * 3
+    lib.focus_window_decode_step_at.restype = ctypes.c_int
     lib.focus_last_error.argtypes = []
     lib.focus_last_error.restype = ctypes.c_char_p
     lib.focus_version.argtypes = []
@@ -458,3 +481,61 @@ def focus_qk_norm_rope_bwd(rp, q, k, q_weight, k_weight, positions, turns, dq_ou
         ctypes.byref(rp), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(positions), _ptr(turns), _ptr(dq_out),
         _ptr(dk_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(dq), _ptr(dk), _ptr(dq_weight),
         _ptr(dk_weight), _stream()))
+
+
+def make_window_params(B, Hq, Hkv, n, d, window, sinks=0, dtype="bf16", scale=0.0, softcap=0.0, packed=False, span_max=0,
+                       q_strides=None, kv_strides=None, o_strides=None):
+    """packed: the B sequences lie in one [1,H,n,d] set of tensors, where the spans of a call say; span_max: the longest span
+    (0: n).  For a decode step n is the capacity of the caches."""
+    arr = lambda st: (ctypes.c_int64 * 3)(*(st if st is not None else (0, 0, 0)))
+    return FocusWindowParams(B, Hq, Hkv, n, d, window, sinks, DTYPES[dtype], 1 if packed else 0, span_max, scale, softcap,
+                             arr(q_strides), arr(kv_strides), arr(o_strides))
+
+
+def _check_spans(p, spans):
+    assert spans is None or (spans.dtype == torch.int32 and spans.is_contiguous() and spans.numel() == 2 * p.B)
+
+
+def focus_window_attn_fwd(p, q, k, v, out, lse=None, spans=None):
+    """spans int32 [B,2] on the device: (first row, length) of every sequence; None: whole rows."""
+    _check_spans(p, spans)
+    _check(load_library().focus_window_attn_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(spans), _ptr(out), _ptr(lse),
+                                                _stream()))
+
+
+def _alloc_sized(fn, p, device):
+    out = ctypes.c_size_t(0)
+    _check(fn(ctypes.byref(p), ctypes.byref(out)))
+    return torch.empty(max(out.value, 256), dtype=torch.uint8, device=device)
+
+
+def alloc_window_bwd_workspace(p, device="cuda"):
+    return _alloc_sized(load_library().focus_window_bwd_workspace_size, p, device)
+
+
+def focus_window_attn_bwd(p, q, k, v, out, lse, dout, workspace, dq, dk, dv, spans=None):
+    _check_spans(p, spans)
+    _check(load_library().focus_window_attn_bwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(dout),
+                                                _ptr(spans), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                                _ptr(dq), _ptr(dk), _ptr(dv), _stream()))
+
+
+def focus_window_cache_fill(p, k, v, k_cache, v_cache, spans=None):
+    """p: of the prompt; the caches [B,Hkv,capacity,d]."""
+    _check_spans(p, spans)
+    assert k_cache.is_contiguous() and v_cache.is_contiguous() and k_cache.shape == v_cache.shape
+    _check(load_library().focus_window_cache_fill(ctypes.byref(p), k_cache.shape[2], _ptr(k), _ptr(v), _ptr(spans),
+                                                  _ptr(k_cache), _ptr(v_cache), _stream()))
+
+
+def alloc_window_decode_workspace(p, device="cuda"):
+    return _alloc_sized(load_library().focus_window_decode_workspace_size, p, device)
+
+
+def focus_window_decode_step_at(p, pos_dev, q_new, k_new, v_new, k_cache, v_cache, workspace, out, lse=None):
+    """One token per sequence at the positions in device memory (int32 [B]); p.n is the capacity of the caches."""
+    assert pos_dev.dtype == torch.int32 and pos_dev.is_cuda and pos_dev.is_contiguous() and pos_dev.numel() == p.B
+    _check(load_library().focus_window_decode_step_at(ctypes.byref(p), _ptr(pos_dev), _ptr(q_new), _ptr(k_new), _ptr(v_new),
+                                                      _ptr(k_cache), _ptr(v_cache), _ptr(workspace),
+                                                      workspace.numel() * workspace.element_size(), _ptr(out), _ptr(lse),
+                                                      _stream()))
