@@ -392,7 +392,8 @@ typedef struct {
     int32_t span_max;          /* longest span (0 selects n); a longer one is cut to it                       */
     float scale;               /* 0 selects 1/sqrt(d)                                                         */
     float softcap;             /* 0 = off                                                                     */
-    int64_t q_strides[3], kv_strides[3], o_strides[3];   /* as in focus_params; dq has q's, dk and dv have kv's, dout has out's */
+    int64_t q_strides[3], kv_strides[3], o_strides[3];   /* as in focus_params; dq has q's, dk and dv have kv's, dout has out's;
+                                  position strides below 2^25 bytes */
 } focus_window_params;
 
 /* spans [B,2] int32 DEVICE, nullable unless packed: sequence b is the rows first .. first + length - 1 (cut to the n rows), its positions count

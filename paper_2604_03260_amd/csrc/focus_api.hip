@@ -1042,6 +1042,9 @@ focus_status make_window_args(const focus_window_params* p, focus::WindowArgs* A
     if (!take_strides(p->q_strides, p->Hq, p->n, p->d, elem, A->qs) || !take_strides(p->kv_strides, p->Hkv, p->n, p->d, elem, A->ks) ||
         !take_strides(p->o_strides, p->Hq, p->n, p->d, elem, A->os))
         return fail(FOCUS_EINVAL, "strides must be >= 0 and multiples of 16 bytes");
+    // (a tile's 64 rows are addressed with 32 bits)
+    for (long long x : {A->qs[2], A->ks[2], A->os[2]})
+        if (x * elem >= (1ll << 25)) return fail(FOCUS_EUNSUPPORTED, "a position stride of 2^25 bytes or more is not built");
     return FOCUS_OK;
 }
 

@@ -5,7 +5,7 @@
 // the first half for their row or column, lanes 32..63 the second.  For 16-bit types that is the operand of one v_mfma 32x32x16; for
 // fp32 its four components go into four v_mfma 32x32x2, whose two contracted indices are then 4 apart, on both operands alike.
 // The result holds, in lane l and register i, column l % 32 and row 8 (i/4) + 4 (l/32) + i % 4.  A result can therefore be
-// the next product's second operand as it is, if the first operand's contracted index is stored in that order (slot_of_row).
+// the next product's second operand as it is, if the first operand's contracted index is taken in that order (comps_piece).
 #pragma once
 #include "focus_internal.h"
 
@@ -16,6 +16,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+#define WINDOW_INLINE __attribute__((always_inline))     // of lambdas: a call would go through memory
 
 constexpr int WTHR = 256;                   // threads of a work-group: four wavefronts
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -99,10 +102,19 @@ template <> struct Piece<float> {
 template <typename T>
 __device__ inline u32x4 load_piece(const T* row, int piece) { return *(const u32x4*)((const char*)row + 16 * piece); }
 
-// A tile of R rows of D components in LDS.
-//   by rows       row r at r * RPITCH, its 16-byte piece c at place c ^ f(r), f(r) = (r ^ r >> 2) & 7: the eight lanes that a 16-byte access serves
-//                 at a time touch all 32 banks, when they read eight consecutive rows and when they write every fourth one
-//   by components component d at d * TPITCH, the R rows in operand order; 16 bytes of padding do the same there
+// A register whose value the compiler cannot see through: addresses derived from it are found where they are used (a few additions)
+// instead of being kept, which cost the kernels below up to 70 spilled registers.
+__device__ inline int opaque(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// A tile of R rows of D components in LDS, the first operand of both kinds of product: by rows (its rows are the product's rows), and by components
+// (its components are; its rows are contracted, four at a time from the LDS reads that turn 4 x 16 values of 16 bits around, one by one for fp32).
+// Row r lies at r * RPITCH, its 16-byte piece c at place c ^ turn(r), so that neither kind of read meets a bank twice: the 16 consecutive rows
+// of a read by rows have 16 different turns (8, where two rows share 256 bytes), and the four rows of a read by components differ
+// in the bits of the turn that choose among the 64-byte quarters.  Tiles start at multiples of 256 bytes.
 template <typename T, int D, int R>
 struct Tile {
     static constexpr int ES = (int)sizeof(T), E = Piece<T>::E;
@@ -110,123 +122,125 @@ struct Tile {
     static constexpr int KS = PIECES / 2;                      // steps of a product over the components
     static constexpr int DB = (D + 31) / 32;                   // blocks of 32 components
     static constexpr int US = 32 / (2 * E);                    // steps of a product over 32 rows
-    static constexpr int RPITCH = round_up(PIECES, 8) * 16;
-    static constexpr int TPITCH = R * ES + 16;
-    static constexpr int RBYTES = R * RPITCH, TBYTES = DB * 32 * TPITCH;
-    static constexpr int BLOCKS = R / 4 * PIECES;              // blocks of 4 rows by one piece: what a thread moves at a time
+    static constexpr int RPITCH = round_up(PIECES, 8) * 16, BLOCK = 32 * RPITCH;       // bytes of a row, of 32 rows
+    static constexpr int BYTES = R * RPITCH;
+    static constexpr int SWAP = RPITCH % 256 == 0 ? 15 : 7;    // places among which a row's pieces change
 
-    static __device__ int row_at(int r, int piece) { return r * RPITCH + (piece >> 3) * 128 + (((piece & 7) ^ ((r ^ (r >> 2)) & 7)) << 4); }
-    // first of four consecutive rows 4g .. 4g+3 in operand order (in rows)
-    static __device__ int slot_of_rows(int g) { return ES == 4 ? 4 * g : (g >> 2) * 16 + (g & 1) * 8 + ((g >> 1) & 1) * 4; }
-
-    // operand of 32 rows (from row 32 * unit), step s over the components
-    static __device__ u32x4 rows_piece(const char* tile, int unit, int s, int lane)
+    static __device__ int turn_of_row(int r) { return SWAP == 15 ? (r & 3) << 2 | ((r >> 2) & 3) : (r & 2) << 1 | ((r >> 2) & 3); }
+    // A lane's place for reads by rows of a block of 32 rows, and the operand of step s over the components: pieces 2s and 2s + 1
+    static __device__ int rows_place(int lane)
     {
-        return *(const u32x4*)(tile + row_at(32 * unit + (lane & 31), 2 * s + (lane >> 5)));
+        const int r = lane & 31, hh = lane >> 5;
+        return r * RPITCH + ((hh ^ turn_of_row(r)) << 4);
     }
-    // operand of 32 components (block db), step s over the rows of 32-row unit `unit`
-    static __device__ u32x4 comps_piece(const char* tile, int db, int unit, int s, int lane)
+    static __device__ u32x4 rows_piece(const char* block, int place, int s)
     {
-        return *(const u32x4*)(tile + (32 * db + (lane & 31)) * TPITCH + 32 * ES * unit + 32 * s + 16 * (lane >> 5));
+        return *(const u32x4*)(block + ((place ^ ((2 * s & SWAP) << 4)) + 16 * (2 * s & ~SWAP)));
     }
-};
-
-// Two tiles on their way from global memory to LDS: every thread holds blocks of 4 rows by 16 bytes.
-template <typename T, int D, int R>
-struct Stage {
-    typedef Tile<T, D, R> TL;
-    static constexpr int N = (2 * TL::BLOCKS + WTHR - 1) / WTHR;
-    u32x4 r[N][4];
-
-    static __device__ void place(int i, int* which, int* rows, int* piece)
+    // The same by components: the operand of components 32 db .. and step s over the 32 rows.  16-bit types: v_mfma slots 0 .. 7 of half-wave h
+    // are rows 16 s + 4 h + {0 .. 3, 8 .. 11}, the order in which a result holds its rows; fp32: row 8 s + 4 h + j for product j.
+    static __device__ int comps_place(int lane)
     {
-        int id = (int)threadIdx.x + WTHR * i;
-        *which = id >= TL::BLOCKS;
-        id -= *which ? TL::BLOCKS : 0;
-        *rows = id % (R / 4);
-        *piece = id / (R / 4);
+        const int hh = lane >> 5, l = lane & 15;
+        if (ES == 4) return 4 * hh * RPITCH + ((((lane & 31) >> 2) ^ hh) << 4) + 4 * (lane & 3);
+        const int r = 4 * hh + l / 4, c = 2 * ((lane >> 4) & 1) + (l & 3) / 2;
+        return r * RPITCH + ((c ^ turn_of_row(r)) << 4) + 8 * (l & 1);
     }
-    // rows row0 .. row0 + R - 1 of a and b (row strides as, bs); zeros at and behind row len
-    __device__ void load(const T* a, long long as, const T* b, long long bs, int row0, int len)
+    static __device__ u32x4 comps_piece(const char* block, int place, int db, int s)
     {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            int which, g, piece;
-            place(i, &which, &g, &piece);
-            if ((2 * TL::BLOCKS) % WTHR != 0 && piece >= TL::PIECES) continue;      // behind the last block
-            const T* p = which ? b : a;
-            const long long st = which ? bs : as;
-            const int row = row0 + 4 * g;
-            p += (long long)row * st;
+        u32x4 x;
+        if constexpr (ES == 4) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                u32x4 x = {0u, 0u, 0u, 0u};
-                if (row + j < len) x = load_piece(p + j * st, piece);
-                r[i][j] = x;
+                const int turn = (SWAP == 15 ? j << 2 : (j & 2) << 1) | 2 * (s & 1);
+                x[j] = *(const unsigned*)(block + ((place ^ ((turn ^ (8 * db & SWAP)) << 4)) + 16 * (8 * db & ~SWAP) + (8 * s + j) * RPITCH));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const char* at = block + ((place ^ (((4 * db & SWAP) ^ 2 * j) << 4)) + 16 * (4 * db & ~SWAP) + (16 * s + 8 * j) * RPITCH);
+                const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+                x[2 * j] = y.x;
+                x[2 * j + 1] = y.y;
             }
         }
+        return x;
     }
-    // tile `which` by rows and by components (null: not in that order)
-    __device__ void store(char* arows, char* acomps, char* brows, char* bcomps) const
+};
+
+// A tile straight from global memory to LDS, 16 bytes a lane: a wavefront's loads fill LDS in order, so a lane fetches the piece that belongs in its
+// place.  WAVES wavefronts share the tile.  Rows behind the last one are that row again (they are hidden by position).  Complete when vmcnt
+// is 0 (dma_wait).  64 rows span less than 2^31 bytes (checked by the host).
+template <typename T, int D, int R, int WAVES>
+struct Dma {
+    typedef Tile<T, D, R> TL;
+    static constexpr int N = TL::BYTES / (1024 * WAVES);      // 1-KB loads of a wavefront
+    static_assert(TL::BYTES % (1024 * WAVES) == 0, "the wavefronts fill a tile with equal numbers of loads");
+    int off[N];                                               // of a lane in a whole tile
+
+    static __device__ int source(int i, int wave, int lane, int pitch, int left)
+    {
+        constexpr int PLACES = TL::RPITCH / 16;
+        const int id = 64 * (wave * N + i) + lane, row = id / PLACES, at = id % PLACES;
+        int piece = at ^ TL::turn_of_row(row);
+        if (TL::PIECES % 8 != 0 && piece >= TL::PIECES) piece = 0;      // (a place that matters to no result)
+        return min(row, left - 1) * pitch + 16 * piece;
+    }
+    __device__ void init(int wave, int lane, int pitch)
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            int which, g, piece;
-            place(i, &which, &g, &piece);
-            if ((2 * TL::BLOCKS) % WTHR != 0 && piece >= TL::PIECES) continue;
-            char* rows = which ? brows : arows;
-            char* comps = which ? bcomps : acomps;
-            if (rows) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *(u32x4*)(rows + TL::row_at(4 * g + j, piece)) = r[i][j];
-            }
-            if (comps) {
-                char* at = comps + piece * TL::E * TL::TPITCH + TL::slot_of_rows(g) * TL::ES;
-                if constexpr (TL::ES == 4) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const u32x4 x = {r[i][0][c], r[i][1][c], r[i][2][c], r[i][3][c]};
-                        *(u32x4*)(at + c * TL::TPITCH) = x;
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint2 lo, hi;                                    // components 2c and 2c + 1 of the four rows
-                        lo.x = __builtin_amdgcn_perm(r[i][1][c], r[i][0][c], 0x05040100u);
-                        lo.y = __builtin_amdgcn_perm(r[i][3][c], r[i][2][c], 0x05040100u);
-                        hi.x = __builtin_amdgcn_perm(r[i][1][c], r[i][0][c], 0x07060302u);
-                        hi.y = __builtin_amdgcn_perm(r[i][3][c], r[i][2][c], 0x07060302u);
-                        *(uint2*)(at + 2 * c * TL::TPITCH) = lo;
-                        *(uint2*)(at + (2 * c + 1) * TL::TPITCH) = hi;
-                    }
-                }
-            }
-        }
+        for (int i = 0; i < N; ++i) off[i] = source(i, wave, lane, pitch, R);
     }
-    // Values that are not finite, in a tile with hidden pairs: a hidden pair's weight is zero, but 0 * inf is not.  They become zeros, and
-    // their rows are marked (bit r of the two words at bad): whoever sees such a row is spoiled as a whole (spoiled_by).
-    __device__ void take_out_not_finite(unsigned* bad)
+    // rows of `pitch` bytes from `rows` on, `left` of them
+    __device__ void load(const T* rows, int pitch, int left, char* tile, int wave, int lane) const
     {
+        const unsigned to = __builtin_amdgcn_readfirstlane(lds_addr_of(tile) + 1024 * N * wave);
+        const uintptr_t from = (uintptr_t)rows;               // (the same in all lanes, in scalar registers)
+        const char* base = (const char*)((uintptr_t)(unsigned)__builtin_amdgcn_readfirstlane((int)from) |
+                                         (uintptr_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(from >> 32)) << 32);
+        if (left >= R) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            int which, g, piece;
-            place(i, &which, &g, &piece);
-            if ((2 * TL::BLOCKS) % WTHR != 0 && piece >= TL::PIECES) continue;
-            unsigned rows = 0;
+            for (int i = 0; i < N; ++i) lds_dma16(base, off[i], to + 1024 * i);
+        } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const unsigned x = r[i][j][c] & Piece<T>::EXP;
-                    unsigned keep = (x & 0xffff0000u) == (Piece<T>::EXP & 0xffff0000u) ? 0u : 0xffffffffu;
-                    if constexpr (TL::ES == 2) keep = (keep & 0xffff0000u) | ((x & 0xffffu) == (Piece<T>::EXP & 0xffffu) ? 0u : 0xffffu);
-                    r[i][j][c] &= keep;
-                    rows |= keep != 0xffffffffu ? 1u << j : 0u;
-                }
-            if (rows) atomicOr(&bad[g >> 3], rows << (4 * (g & 7)));
+            for (int i = 0; i < N; ++i) lds_dma16(base, source(i, wave, lane, pitch, left), to + 1024 * i);
         }
     }
 };
+__device__ inline void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Values that are not finite, in a tile that some row does not see as a whole: the weight of what is hidden is zero, but 0 * inf is not.  They
+// become zeros, and their rows are marked (bit r of the two words at bad): whoever sees such a row is spoiled as a whole (spoiled_by).
+// By all threads of the work-group, between two barriers.
+template <typename T, int D, int R>
+__device__ inline void scrub(char* tile, unsigned* bad)
+{
+    typedef Tile<T, D, R> TL;
+    for (int id = threadIdx.x; id < TL::BYTES / 16; id += WTHR) {
+        u32x4 v = *(const u32x4*)(tile + 16 * id);
+        bool found = false;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const unsigned x = v[c] & Piece<T>::EXP;
+            unsigned keep = (x & 0xffff0000u) == (Piece<T>::EXP & 0xffff0000u) ? 0u : 0xffffffffu;
+            if constexpr (TL::ES == 2) keep = (keep & 0xffff0000u) | ((x & 0xffffu) == (Piece<T>::EXP & 0xffffu) ? 0u : 0xffffu);
+            found |= keep != 0xffffffffu;
+            v[c] &= keep;
+        }
+        if (found) {
+            const int row = id / (TL::RPITCH / 16);
+            *(u32x4*)(tile + 16 * id) = v;
+            atomicOr(&bad[row >> 5], 1u << (row & 31));
+        }
+    }
+}
+
+// A wavefront's LDS accesses take effect in order: between its own writes and reads only the compiler has to be kept to it.
+__device__ inline void own_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
 // A sequence of a call: its length and the element offsets of its first row.
 struct Sequence {
@@ -247,11 +261,16 @@ __device__ inline Sequence sequence_of(const WindowArgs& A, int b)
     return s;
 }
 
-// The other half-wave's value: lanes l and l ^ 32 hold halves of one column
-__device__ inline float other_half(float x)
+// Lanes l and l ^ 32 hold halves of one column: the largest, the sum of their values
+__device__ inline float halves_max(float x)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float halves_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // What a block of 32 rows and 32 keys (positions row0.., key0..) needs
@@ -265,7 +284,8 @@ __device__ inline Block block_kind(int row0, int key0, int window, int sinks)
 }
 __device__ inline bool visible(int row, int key, int window, int sinks)
 {
-    return (unsigned)(row - key) < (unsigned)window || (key < sinks && key <= row);
+    // (bitwise: as a chain of conditions it became branches, 32 of them in a block)
+    return (bool)((int)((unsigned)(row - key) < (unsigned)window) | ((int)(key < sinks) & (int)(key <= row)));
 }
 
 // Does a lane's row (or key) see a marked one of the 32 keys (rows) at `other`?  marks: the 32 bits of that block; kept by the half-wave that holds
@@ -274,11 +294,12 @@ template <bool KEYS_MARKED>
 __device__ inline bool spoiled_by(unsigned marks, int mine, int other, int hh, int window, int sinks)
 {
     bool hit = false;
+    mine = opaque(mine);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int at = 8 * (i / 4) + 4 * hh + i % 4;
         const bool seen = KEYS_MARKED ? visible(mine, other + at, window, sinks) : visible(other + at, mine, window, sinks);
-        hit |= seen && ((marks >> at) & 1u);
+        hit |= (bool)((int)seen & (int)((marks >> at) & 1u));
     }
     return hit;
 }
@@ -302,6 +323,61 @@ __device__ inline void store_row(T* row, const f32x16* acc, float f, int lane)
             if constexpr (sizeof(T) == 4) *(u32x4*)at = p;
             else { uint2 y; y.x = p[0]; y.y = p[1]; *(uint2*)at = y; }
         }
+}
+
+// The keys that rows first .. last can see, in blocks of 32 and tiles of U blocks: the sinks' blocks, then those from the first key of the
+// window on.  (The last tile of the sinks may have fewer blocks, so that none is walked for nothing.)
+struct Walk {
+    int first, last, sink_blocks, sink_tiles, base, blocks, tiles;
+    int lone_tile;              // the last tile of the sinks if it has one block where others have two: no step between its first and its last
+    int open0;                  // keys from here to the first row hide nothing
+    __device__ Walk(const WindowArgs& A, const Sequence& sq, int first_, int last_, int U)
+    {
+        first = first_;
+        last = last_;
+        sink_blocks = (min(A.sinks, last + 1) + 31) / 32;
+        sink_tiles = (sink_blocks + U - 1) / U;
+        base = max(32 * sink_blocks, max(0, first - A.window + 1) & ~31);
+        const int near = max(0, last / 32 - base / 32 + 1);
+        blocks = sink_blocks + near;
+        tiles = sink_tiles + (near + U - 1) / U;
+        lone_tile = U == 2 && sink_blocks % 2 != 0 ? sink_tiles - 1 : -1;
+        open0 = last - A.window + 1;
+    }
+    // may a pair of the rows and keys key0 .. key0 + R - 1 be hidden?
+    __device__ bool edge(int key0, int R, const WindowArgs& A) const
+    {
+        return key0 + R - 1 > first || (key0 < open0 && key0 + R - 1 >= A.sinks);
+    }
+};
+
+// tanh of 16 scores times f: its series to z^9 while all are below 0.3 in magnitude (the next term is 1.6e-8 there, half a step of fp32
+// relative to z: six operations in place of an exponential and a reciprocal), else from exp(-2 |z|); fp32 takes the library's there.
+template <typename T>
+__device__ inline void tanh_scores(f32x16& x, float f)
+{
+    float big = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        x[i] *= f;
+        big = fmaxf(big, fabsf(x[i]));
+    }
+    if (!__any(!(big <= 0.3f))) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float z = x[i], w = z * z;
+            x[i] = fmaf(z * w, fmaf(w, fmaf(w, fmaf(w, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), z);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if constexpr (sizeof(T) == 4) x[i] = tanhf(x[i]);
+            else {
+                const float e = __builtin_amdgcn_exp2f(-2.f * LOG2E * fabsf(x[i]));
+                x[i] = copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x[i]);
+            }
+        }
+    }
 }
 
 // The place of a work-group: consecutive ones go to the eight XCDs in turn, and each XCD gets a contiguous share of the work, so that

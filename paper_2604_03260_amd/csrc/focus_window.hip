@@ -4,14 +4,19 @@
 //   S^T = K Q^T  (A = keys by rows, B = the wavefront's 32 queries, held in registers)
 //   P^T = exp2(scale' S^T - m), one row of the softmax per lane (and half-wave), so its maximum and sum are sums in a lane
 //   O^T += V^T P^T (A = values by components; P^T is the B operand as the first product left it, focus_window.h)
-// A work-group is four wavefronts of 32 rows each that share the staged keys: of up to four query heads of one KV head (the same rows: the
-// four walk in step and the walk is as short as the window allows), else of consecutive rows.  Keys come through registers
-// (the next tile's loads are on their way during the products of this one); values are turned there (16 v_perm per 4 x 8 components), so
-// no copy of them in another order is needed and the call is one launch without workspace.
+// A work-group is four wavefronts that share the staged keys; each owns 32 rows of one query head.  The heads of a KV head come first, then
+// the next rows: with four heads all four walk in step, and the walk is as short as the window allows.  Keys and values go straight to
+// LDS; the values' rows are turned by the LDS reads, so no copy of them in another order is needed and the call is one launch without
+// workspace.  (Turned in registers on their way, 16 v_perm and 8 stores per 4 x 8 components, they took a fifth of the time.)
+// A wavefront's walk is a sequence of blocks of 32 keys, one step each, in which the vector units and the matrix cores have independent work:
+//   step i:  softmax of block i  beside  S of block i + 1 and O += V P of block i - 1
+// so K is a block ahead of the softmax and V a block behind it, both in two buffers, with one barrier per tile.
 // The reference m of a row moves only when its maximum has risen by more than 8 (log2 units): O is rarely rescaled, and the
 // probabilities stay below 2^8.  IEEE halves lose bits below 2^-14: there the reference lies 6 lower, so what is dropped is below 2^-31 of the
 // largest, 2^-11 of the sum over 2^20 keys.
 #include "focus_window.h"
+
+#include <type_traits>
 
 namespace focus {
 
@@ -24,30 +29,29 @@ template <typename T, int D> constexpr int key_tile() { return sizeof(T) == 4 ||
 template <typename T, int D> constexpr int fwd_waves() { return D * (int)sizeof(T) > 384 ? 1 : 2; }
 
 template <typename T, int D, bool CAP>
-__global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(WindowArgs A, int tiles, int heads, const T* __restrict__ q,
+__global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(WindowArgs A, int blocks, const T* __restrict__ q,
                                                                              const T* __restrict__ k, const T* __restrict__ v,
                                                                              T* __restrict__ out, float* __restrict__ lse)
 {
-    constexpr int R = key_tile<T, D>();
+    constexpr int R = key_tile<T, D>(), U = R / 32;           // keys and steps of a tile
+    constexpr int VLAG = U == 2 ? 1 : 2;                      // tiles that V is fetched behind K
     typedef Tile<T, D, R> TL;
     typedef Piece<T> P;
-    __shared__ __attribute__((aligned(16))) char s_k[TL::RBYTES];
-    __shared__ __attribute__((aligned(16))) char s_v[TL::TBYTES];
-    __shared__ unsigned s_bad[2][2];
+    __shared__ __attribute__((aligned(256))) char s_k[2][TL::BYTES], s_v[2][TL::BYTES];
+    __shared__ unsigned s_bad[4][2];
     const int lane = threadIdx.x & 63, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-    // (b, KV head, tile of rows, share of the query heads), the last one fastest
-    const int G = A.Hq / A.Hkv, shares = G / heads, subs = 4 / heads;
-    const long long w = work_of((long long)A.B * A.Hkv * tiles * shares);
+    // (b, KV head, four of the (rows, query head) of it, the head fastest)
+    const int G = A.Hq / A.Hkv, fours = (blocks * G + 3) / 4;
+    const long long w = work_of((long long)A.B * A.Hkv * fours);
     if (w < 0) return;
-    const int share = (int)(w % shares), tile = (int)(w / shares % tiles), hk = (int)(w / shares / tiles % A.Hkv);
-    const int b = (int)(w / shares / tiles / A.Hkv);
+    const int four = (int)(w % fours), hk = (int)(w / fours % A.Hkv), b = (int)(w / fours / A.Hkv);
     const Sequence sq = sequence_of(A, b);
-    const int tile0 = tile * 32 * subs;                       // first row of the work-group, of the wavefront
+    const int tile0 = four * 4 / G * 32;                      // first row of the work-group
     if (tile0 >= sq.len) return;
-    const int row0 = tile0 + 32 * (wave % subs);
-    const int h = hk * G + share * heads + wave / subs;
+    const int row0 = (four * 4 + wave) / G * 32;              // of the wavefront
+    const int h = hk * G + (four * 4 + wave) % G;
     const int row = row0 + (lane & 31);
     const bool real = row < sq.len;
     const T* qrow = q + (long long)sq.tb * A.qs[0] + (long long)h * A.qs[1] + (long long)(sq.first + (real ? row : sq.len - 1)) * A.qs[2];
@@ -60,76 +64,150 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
     f32x16 o[TL::DB];
 #pragma unroll
     for (int i = 0; i < TL::DB; ++i) o[i] = 0.f;
-    constexpr float LOWER = sizeof(T) == 4 ? 0.f : P::EXP == 0x7c007c00u ? 6.f : 0.f;       // IEEE halves, see above
+    constexpr float LOWER = P::EXP == 0x7c007c00u ? 6.f : 0.f;          // IEEE halves, see above
     float m = -1e30f, l = 0.f;
     const float c = CAP ? A.softcap * LOG2E : A.scale * LOG2E;
     const float ci = CAP ? A.scale / A.softcap : 0.f;
 
-    // tiles with sinks, then those from the first key of the window on
-    const int last = min(tile0 + 32 * subs, sq.len) - 1;
-    const int sink_tiles = (min(A.sinks, last + 1) + R - 1) / R;
-    const int near0 = max(sink_tiles, max(0, tile0 - A.window + 1) / R);
-    const int count = sink_tiles + max(0, last / R - near0 + 1);
-    auto tile_at = [&](int t) { return (t < sink_tiles ? t : near0 + t - sink_tiles) * R; };
-
-    if (threadIdx.x < 4) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
-    Stage<T, D, R> st;
-    st.load(kb, A.ks[2], vb, A.ks[2], tile_at(0), sq.len);
-    for (int t = 0; t < count; ++t) {
-        const int key0 = tile_at(t);
-        const bool edge = key0 + R - 1 > tile0 || (last - key0 >= A.window && key0 + R - 1 >= A.sinks);
-        __syncthreads();                                      // the tile before has been read
-        if (edge) st.take_out_not_finite(s_bad[t & 1]);
-        if (threadIdx.x < 2) s_bad[(t + 1) & 1][threadIdx.x] = 0u;
-        st.store(s_k, nullptr, nullptr, s_v);
-        __syncthreads();
-        if (t + 1 < count) st.load(kb, A.ks[2], vb, A.ks[2], tile_at(t + 1), sq.len);
-
-#pragma unroll 1
-        for (int u = 0; u < R / 32; ++u) {
-            const Block kind = block_kind(row0, key0 + 32 * u, A.window, A.sinks);
-            if (kind == HIDDEN) continue;
-            f32x16 x = 0.f;
-#pragma unroll
-            for (int s = 0; s < TL::KS; ++s) x = P::mma(TL::rows_piece(s_k, u, s, lane), qf[s], x);
-            if (CAP) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = tanhf(x[i] * ci);
-            }
-            if (kind == EDGE) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    x[i] = visible(row, key0 + 32 * u + 8 * (i / 4) + 4 * hh + i % 4, A.window, A.sinks) ? x[i] : -INFINITY;
-            }
-            float top = x[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-            top = fmaxf(top, other_half(top)) * c;
-            if (__any(top > m + LOWER + 8.f)) {
-                const float to = fmaxf(m, top - LOWER), f = exp2f(m - to);
-                m = to;
-                l *= f;
-#pragma unroll
-                for (int i = 0; i < TL::DB; ++i) o[i] *= f;
-            }
-            float p[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -m));
-                l += p[i];
-            }
-            u32x4 pf[TL::US];
-#pragma unroll
-            for (int s = 0; s < TL::US; ++s) pf[s] = P::pack(p + s * P::E);
-#pragma unroll
-            for (int s = 0; s < TL::US; ++s)
-#pragma unroll
-                for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(TL::comps_piece(s_v, db, u, s, lane), pf[s], o[db]);
-            const unsigned marks = s_bad[t & 1][u];
-            if (edge && marks != 0u && spoiled_by<true>(marks, row, key0 + 32 * u, hh, A.window, A.sinks)) l = __builtin_nanf("");
+    const Walk W(A, sq, tile0, min((four * 4 + 3) / G * 32 + 32, sq.len) - 1, U);
+    auto key_at = [&](int t) WINDOW_INLINE { return t < W.sink_tiles ? t * R : W.base + (t - W.sink_tiles) * R; };
+    const int pitch = (int)(A.ks[2] * (long long)sizeof(T));
+    Dma<T, D, R, 4> dma;
+    dma.init(wave, lane, pitch);
+    // (behind the last tile: its rows again, in bounds and never used)
+    auto fetch = [&](const T* base, char* bufs, int t) WINDOW_INLINE {
+        const int key = key_at(min(t, W.tiles - 1));
+        dma.load(base + (long long)key * A.ks[2], pitch, sq.len - key, bufs + (t & 1) * TL::BYTES, wave, lane);
+    };
+    // in the last step of tile t: the next K and V on their way
+    auto turn = [&](int t) WINDOW_INLINE {
+        fetch(kb, s_k[0], t + 2);
+        fetch(vb, s_v[0], t + 2 - VLAG);
+    };
+    // V of tile t has landed and is about to be met
+    auto check = [&](int t) WINDOW_INLINE {
+        if (threadIdx.x < 2) s_bad[(t + 1) & 3][threadIdx.x] = 0u;
+        if (t >= 0 && W.edge(key_at(t), R, A)) {
+            scrub<T, D, R>(s_v[t & 1], s_bad[t & 3]);
+            __syncthreads();
         }
+    };
+    if (threadIdx.x < 8) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
+    for (int i = threadIdx.x; i < TL::BYTES / 16; i += WTHR) *(u32x4*)(s_v[1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};   // (met by weights of zero before it is filled)
+    fetch(kb, s_k[0], 0);
+    fetch(kb, s_k[0], 1);
+    if constexpr (U == 2) fetch(vb, s_v[0], 0);
+    dma_wait();
+    __syncthreads();
+
+    const int rplace = TL::rows_place(lane), cplace = TL::comps_place(lane);
+    f32x16 x = 0.f;                                           // scores of the step's block, then of the next one
+    u32x4 pf[TL::US];                                         // probabilities of the block before
+#pragma unroll
+    for (int s = 0; s < TL::US; ++s) pf[s] = 0u;
+    // hides what a row does not see, once the scores are there (blocks from key open0 to open1 hide nothing)
+    const int open0 = row0 + 32 - A.window, open1 = row0 - 31;
+    auto finish = [&](int key0) WINDOW_INLINE {
+        if (CAP) tanh_scores<T>(x, ci);
+        if (key0 >= open0 && key0 <= open1) return;
+        if (block_kind(row0, key0, A.window, A.sinks) == OPEN) return;
+        const int key = opaque(key0 + 4 * hh);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = visible(row, key + 8 * (i / 4) + i % 4, A.window, A.sinks) ? x[i] : -INFINITY;
+    };
+    // the values of a block, in tile t, place u, have been met: were there marked ones among them?
+    auto look = [&](int t, int u) WINDOW_INLINE {
+        const int key = key_at(t);
+        if (!W.edge(key, R, A)) return;
+        const unsigned marks = s_bad[t & 3][u];
+        if (marks != 0u && spoiled_by<true>(marks, row, key + 32 * u, hh, A.window, A.sinks)) l = __builtin_nanf("");
+    };
+    int tv = 1, uv = 0;                                       // tile and place of the block before (at first: the zeros)
+    // softmax of the scores x beside the next block's scores (K at kbuf) and the last block's values (V at vbuf).  The operands' reads first,
+    // then the softmax, then the products: the reads pass under the softmax, the products of one wavefront of a SIMD under the softmax
+    // of the other
+    auto products = [&](const char* kbuf, const char* vbuf) WINDOW_INLINE {
+        const int rp = opaque(rplace), cp = opaque(cplace);
+        u32x4 va[TL::US * TL::DB], ka[TL::KS];
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+            for (int db = 0; db < TL::DB; ++db) va[s * TL::DB + db] = TL::comps_piece(vbuf, cp, db, s);
+#pragma unroll
+        for (int s = 0; s < TL::KS; ++s) ka[s] = TL::rows_piece(kbuf, rp, s);
+        __builtin_amdgcn_sched_barrier(0);
+        float top = x[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) top = fmaxf(top, x[j]);
+        top = halves_max(top) * c;
+        const bool over = top > m + (LOWER + 8.f), rescale = __any(over);
+        const float to = over ? top - LOWER : m, f = __builtin_amdgcn_exp2f(m - to);      // (a row's bits do not depend on its neighbours)
+        m = to;
+        l *= f;
+        u32x4 pn[TL::US];
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s) {
+            float p[8];
+#pragma unroll
+            for (int j = 0; j < P::E; ++j) {
+                p[j] = __builtin_amdgcn_exp2f(fmaf(x[s * P::E + j], c, -m));
+                l += p[j];
+            }
+            pn[s] = P::pack(p);
+            asm volatile("" : "+v"(pn[s]));                   // (found here, not behind the products)
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+            for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(va[s * TL::DB + db], pf[s], o[db]);
+        x = 0.f;
+#pragma unroll
+        for (int s = 0; s < TL::KS; ++s) x = P::mma(ka[s], qf[s], x);
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s) pf[s] = pn[s];
+        __builtin_amdgcn_sched_barrier(0);
+        if (rescale) {
+#pragma unroll
+            for (int j = 0; j < TL::DB; ++j) o[j] *= f;
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < TL::KS; ++s) x = P::mma(TL::rows_piece(s_k[0], rplace, s), qf[s], x);
+    finish(key_at(0));
+    int t = 0, u = 0;
+#pragma unroll 1
+    for (int i = 0; i < W.blocks; ++i) {
+        const bool lone = t == W.lone_tile, end = u == U - 1 || lone;
+        if (end) {
+            dma_wait();
+            __syncthreads();
+            check(U == 2 ? t : t - 1);
+            if (!lone) turn(t);
+        }
+        const int tk = end ? t + 1 : t, uk = end ? 0 : u + 1;           // (behind the last block: whatever is there, not used)
+        products(s_k[0] + (tk & 1) * TL::BYTES + TL::BLOCK * uk, s_v[0] + (tv & 1) * TL::BYTES + TL::BLOCK * uv);
+        finish(key_at(tk) + 32 * uk);
+        if (i > 0) look(tv, uv);
+        if (lone) {                                           // (this step has read the buffer that the next V goes to)
+            __syncthreads();
+            turn(t);
+        }
+        tv = t;
+        uv = u;
+        t = tk;
+        u = uk;
     }
-    l += other_half(l);
+    dma_wait();                                               // (nothing may land in LDS after the work-group's end)
+    __syncthreads();
+    check(tv);
+    if (row0 >= sq.len) return;
+#pragma unroll
+    for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+        for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(TL::comps_piece(s_v[0] + (tv & 1) * TL::BYTES + TL::BLOCK * uv, cplace, db, s), pf[s], o[db]);
+    look(tv, uv);
+    l = halves_sum(l);
     T* orow = real ? out + (long long)sq.tb * A.os[0] + (long long)h * A.os[1] + (long long)(sq.first + row) * A.os[2] : nullptr;
     store_row<T, D>(orow, o, 1.f / l, lane);
     if (lse && real && hh == 0) lse[((long long)sq.tb * A.Hq + h) * A.n + sq.first + row] = (m + log2f(l)) * LN2;
@@ -138,11 +216,10 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
 template <typename T, int D, bool CAP>
 hipError_t launch_cap(const WindowArgs& A, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st)
 {
-    const int G = A.Hq / A.Hkv, heads = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1, rows = 32 * (4 / heads);
-    const int tiles = (A.span_max + rows - 1) / rows;
-    const long long groups = work_groups((long long)A.B * A.Hkv * tiles * (G / heads));
+    const int G = A.Hq / A.Hkv, blocks = (A.span_max + 31) / 32;
+    const long long groups = work_groups((long long)A.B * A.Hkv * ((blocks * G + 3) / 4));
     if (groups > 0x7fffffffll) return hipErrorInvalidConfiguration;
-    window_fwd_kernel<T, D, CAP><<<(unsigned)groups, WTHR, 0, st>>>(A, tiles, heads, (const T*)q, (const T*)k, (const T*)v, (T*)out, lse);
+    window_fwd_kernel<T, D, CAP><<<(unsigned)groups, WTHR, 0, st>>>(A, blocks, (const T*)q, (const T*)k, (const T*)v, (T*)out, lse);
     return hipGetLastError();
 }
 template <typename T, int D>

@@ -20,20 +20,22 @@ using namespace window;
 
 namespace {
 
-template <typename T, int D> constexpr int bwd_tile() { return sizeof(T) == 4 || D > 128 ? 32 : 64; }
+// Keys of a dq tile: 32, so that two work-groups share a compute unit's LDS.  Rows of a dkv tile: its operands leave room for one wavefront per
+// SIMD only, and one work-group may have all of LDS.
+constexpr int DQ_TILE = 32;
+template <typename T, int D> constexpr int dkv_tile() { return sizeof(T) == 4 || D > 128 ? 32 : 64; }
 template <typename T, int D> constexpr int dq_waves() { return D * (int)sizeof(T) > 256 ? 1 : 2; }
-template <typename T, int D> constexpr int dkv_waves() { return D * (int)sizeof(T) > 128 ? 1 : 2; }
 
 constexpr int KEYS = 128;                   // keys of a dkv work-group
-constexpr int FAR_KEYS = 64;                // ... of a far one: two blocks of 32, each by two wavefronts that share the rows
+constexpr int FAR_KEYS = 32;                // ... of a far one, whose wavefronts share the rows
 
 // Where the sums of the sinks lie in the workspace, and how the far rows are cut.
 struct FarPlan {
     int any;                                // some rows may see sinks behind their window
     int near_tiles;                         // key tiles of 128 that hold sinks
-    int blocks;                             // blocks of 64 sinks
+    int blocks;                             // blocks of 32 sinks
     int chunk, chunks;                      // rows of a chunk (a multiple of 64); chunks of the longest span
-    size_t off_near, off_far, total;        // [B,Hkv,near_tiles][2][128][d], [B,Hkv,blocks,G,chunks,2][2][64][d], bytes from the workspace's base
+    size_t off_near, off_far, total;        // [B,Hkv,near_tiles][2][128][d], [B,Hkv,blocks,G,chunks][2][32][d], bytes from the workspace's base
 };
 
 FarPlan far_plan(const WindowArgs& A)
@@ -46,60 +48,49 @@ FarPlan far_plan(const WindowArgs& A)
         const int G = A.Hq / A.Hkv;
         f.near_tiles = (std::min(A.sinks, A.span_max) + KEYS - 1) / KEYS;
         f.blocks = (std::min(A.sinks, A.span_max) + FAR_KEYS - 1) / FAR_KEYS;
-        // about two work-groups for each compute unit, of 512 rows at least
+        // about two work-groups for each compute unit, of 256 rows at least
         const long long whole = (long long)A.B * A.Hq * f.blocks;
         const int want = (int)std::max(1ll, 512 / std::max(1ll, whole));
-        f.chunk = std::max(512, round_up((A.span_max + want - 1) / want, 64));
+        f.chunk = std::max(256, round_up((A.span_max + want - 1) / want, 64));
         f.chunks = (A.span_max + f.chunk - 1) / f.chunk;
         f.off_near = off;
         off += (size_t)A.B * A.Hkv * f.near_tiles * 2 * KEYS * A.d * sizeof(float);
         f.off_far = off;
-        off += (size_t)A.B * A.Hkv * f.blocks * G * f.chunks * 2 * 2 * FAR_KEYS * A.d * sizeof(float);
+        off += (size_t)A.B * A.Hkv * f.blocks * G * f.chunks * 2 * FAR_KEYS * A.d * sizeof(float);
     }
     f.total = off;
     return f;
 }
 
-// first far row of the keys of near tile `tile`: the near walk ends with the row tile that holds the last row of the window
-template <int R> __host__ __device__ int far_start(int tile, int window) { return ((tile * KEYS + KEYS - 1 + window - 1) / R + 1) * R; }
-
-// P and dS of one lane's 16 pairs: x holds the scores, dp the products of dout and V; seen: pairs that are not visible give zeros
-template <bool CAP>
-__device__ inline float prob(float x, float c, float ci, float lse2, float* t)
-{
-    if (CAP) {
-        *t = tanhf(x * ci);
-        return __builtin_amdgcn_exp2f(fmaf(*t, c, -lse2));
-    }
-    return __builtin_amdgcn_exp2f(fmaf(x, c, -lse2));
-}
+// first far row of the keys of near tile `tile`: the near walk ends with the block of 32 rows that holds the last row of the window
+__host__ __device__ inline int far_start(int tile, int window) { return ((tile * KEYS + KEYS - 1 + window - 1) / 32 + 1) * 32; }
 
 template <typename T, int D, bool CAP>
-__global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(WindowArgs A, int tiles, int heads, const T* __restrict__ q,
+__global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(WindowArgs A, int blocks, const T* __restrict__ q,
                                                                            const T* __restrict__ k, const T* __restrict__ v,
                                                                            const T* __restrict__ out, const float* __restrict__ lse,
                                                                            const T* __restrict__ dout, float* __restrict__ delta,
                                                                            T* __restrict__ dq)
 {
-    constexpr int R = bwd_tile<T, D>();
+    constexpr int R = DQ_TILE;
     typedef Tile<T, D, R> TL;
     typedef Piece<T> P;
-    __shared__ __attribute__((aligned(16))) char s_k[TL::RBYTES];
-    __shared__ __attribute__((aligned(16))) char s_kc[TL::TBYTES];
-    __shared__ __attribute__((aligned(16))) char s_v[TL::RBYTES];
-    __shared__ unsigned s_bad[2][2];
+    constexpr bool ROWS = D * (int)sizeof(T) <= 512;          // longer rows do not fit LDS often enough: by rows they are read from L1
+    constexpr int NK = ROWS ? 4 : 2;                          // K from a step before its scores to a step behind its dS
+    __shared__ __attribute__((aligned(256))) char s_k[NK][TL::BYTES];
+    __shared__ __attribute__((aligned(256))) char s_v[ROWS ? 2 : 1][ROWS ? TL::BYTES : 256];
+    __shared__ unsigned s_bad[4][2];
     const int lane = threadIdx.x & 63, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int G = A.Hq / A.Hkv, shares = G / heads, subs = 4 / heads;
-    const long long w = work_of((long long)A.B * A.Hkv * tiles * shares);
+    const int G = A.Hq / A.Hkv, fours = (blocks * G + 3) / 4;
+    const long long w = work_of((long long)A.B * A.Hkv * fours);
     if (w < 0) return;
-    const int share = (int)(w % shares), tile = (int)(w / shares % tiles), hk = (int)(w / shares / tiles % A.Hkv);
-    const int b = (int)(w / shares / tiles / A.Hkv);
+    const int four = (int)(w % fours), hk = (int)(w / fours % A.Hkv), b = (int)(w / fours / A.Hkv);
     const Sequence sq = sequence_of(A, b);
-    const int tile0 = tile * 32 * subs;
+    const int tile0 = four * 4 / G * 32;
     if (tile0 >= sq.len) return;
-    const int row0 = tile0 + 32 * (wave % subs);
-    const int h = hk * G + share * heads + wave / subs;
+    const int row0 = (four * 4 + wave) / G * 32;
+    const int h = hk * G + (four * 4 + wave) % G;
     const int row = row0 + (lane & 31);
     const bool real = row < sq.len;
     const int at = sq.first + (real ? row : sq.len - 1);
@@ -117,7 +108,7 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
         gf[s] = load_piece(dout + ooff, 2 * s + hh);
         del += P::dot(gf[s], load_piece(out + ooff, 2 * s + hh));
     }
-    del += other_half(del);
+    del = halves_sum(del);
     if (real && hh == 0) delta[li] = del;
     const float lse2 = lse[li] * LOG2E;
     float spoiled = 0.f;                                      // or NaN
@@ -127,119 +118,203 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
     const float c = CAP ? A.softcap * LOG2E : A.scale * LOG2E;
     const float ci = CAP ? A.scale / A.softcap : 0.f;
 
-    const int last = min(tile0 + 32 * subs, sq.len) - 1;
-    const int sink_tiles = (min(A.sinks, last + 1) + R - 1) / R;
-    const int near0 = max(sink_tiles, max(0, tile0 - A.window + 1) / R);
-    const int count = sink_tiles + max(0, last / R - near0 + 1);
-    auto tile_at = [&](int t) { return (t < sink_tiles ? t : near0 + t - sink_tiles) * R; };
+    const int rplace = TL::rows_place(lane), cplace = TL::comps_place(lane);
+    // the forward kernel's walk with tiles of one block; step i: S and dP of block i + 1, dS of block i, dQ += dS K of block i - 1
+    const Walk W(A, sq, tile0, min((four * 4 + 3) / G * 32 + 32, sq.len) - 1, 1);
+    auto key_at = [&](int t) WINDOW_INLINE { return t < W.sink_tiles ? t * R : W.base + (t - W.sink_tiles) * R; };
+    const int pitch = (int)(A.ks[2] * (long long)sizeof(T));
+    Dma<T, D, R, 4> dma;
+    dma.init(wave, lane, pitch);
+    auto fetch = [&](const T* base, char* buf, int t) WINDOW_INLINE {
+        const int key = key_at(min(t, W.tiles - 1));
+        dma.load(base + (long long)key * A.ks[2], pitch, sq.len - key, buf, wave, lane);
+    };
+    auto fetch_both = [&](int t) WINDOW_INLINE {
+        fetch(kb, s_k[0] + (t & (NK - 1)) * TL::BYTES, t);
+        if constexpr (ROWS) fetch(vb, s_v[0] + (t & 1) * TL::BYTES, t);
+    };
+    // K of tile t has landed and is about to be met
+    auto check = [&](int t) WINDOW_INLINE {
+        if (threadIdx.x < 2) s_bad[(t + 1) & 3][threadIdx.x] = 0u;
+        if (t >= 0 && t < W.tiles && W.edge(key_at(t), R, A)) {
+            scrub<T, D, R>(s_k[0] + (t & (NK - 1)) * TL::BYTES, s_bad[t & 3]);
+            __syncthreads();
+        }
+    };
+    if (threadIdx.x < 8) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
+    for (int i = threadIdx.x; i < TL::BYTES / 16; i += WTHR) *(u32x4*)(s_k[NK - 1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};
+    if constexpr (ROWS) {
+        fetch_both(0);
+        fetch_both(1);
+    }
+    dma_wait();
+    __syncthreads();
+    if constexpr (ROWS) check(0);
 
-    if (threadIdx.x < 4) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
-    Stage<T, D, R> st;
-    st.load(kb, A.ks[2], vb, A.ks[2], tile_at(0), sq.len);
-    for (int t = 0; t < count; ++t) {
-        const int key0 = tile_at(t);
-        const bool edge = key0 + R - 1 > tile0 || (last - key0 >= A.window && key0 + R - 1 >= A.sinks);
+    auto scores = [&](int t, f32x16& z, f32x16& dz) WINDOW_INLINE {
+        const int rp = opaque(rplace), r = min(key_at(t) + (lane & 31), sq.len - 1);
+        const char *kbuf = s_k[0] + (t & (NK - 1)) * TL::BYTES, *vbuf = s_v[0] + (ROWS ? (t & 1) * TL::BYTES : 0);
+        z = 0.f;
+        dz = 0.f;
+#pragma unroll
+        for (int s = 0; s < TL::KS; ++s) {
+            z = P::mma(ROWS ? TL::rows_piece(kbuf, rp, s) : load_piece(kb + (long long)r * A.ks[2], 2 * s + hh), qf[s], z);
+            dz = P::mma(ROWS ? TL::rows_piece(vbuf, rp, s) : load_piece(vb + (long long)r * A.ks[2], 2 * s + hh), gf[s], dz);
+        }
+    };
+    f32x16 x, dx;
+    u32x4 pf[TL::US];
+#pragma unroll
+    for (int s = 0; s < TL::US; ++s) pf[s] = 0u;
+    // soft-caps the scores and hides what a row does not see: exponents of -inf, and dP = delta, so that dS is zero whatever was there
+    const int open0 = row0 + 32 - A.window, open1 = row0 - 31;           // blocks from key open0 to open1 hide nothing
+    auto finish = [&](int key0) WINDOW_INLINE {
+        if (CAP) tanh_scores<T>(x, ci);
+        if (key0 >= open0 && key0 <= open1) return;
+        if (block_kind(row0, key0, A.window, A.sinks) == OPEN) return;
+        const int key = opaque(key0 + 4 * hh);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool seen = visible(row, key + 8 * (i / 4) + i % 4, A.window, A.sinks);
+            x[i] = seen ? x[i] : CAP ? -1e30f : -INFINITY;
+            dx[i] = seen ? dx[i] : 0.f;
+        }
+    };
+    auto look = [&](int t) WINDOW_INLINE {
+        const int key = key_at(t);
+        if (!W.edge(key, R, A)) return;
+        const unsigned marks = s_bad[t & 3][0];
+        if (marks != 0u && spoiled_by<true>(marks, row, key, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
+    };
+    constexpr bool AHEAD = ROWS && D * (int)sizeof(T) <= 256;           // (registers)
+    auto step = [&](int i) WINDOW_INLINE {
+        dma_wait();
         __syncthreads();
-        if (edge) st.take_out_not_finite(s_bad[t & 1]);
-        if (threadIdx.x < 2) s_bad[(t + 1) & 1][threadIdx.x] = 0u;
-        st.store(s_k, s_kc, s_v, nullptr);
-        __syncthreads();
-        if (t + 1 < count) st.load(kb, A.ks[2], vb, A.ks[2], tile_at(t + 1), sq.len);
-#pragma unroll 1
-        for (int u = 0; u < R / 32; ++u) {
-            const Block kind = block_kind(row0, key0 + 32 * u, A.window, A.sinks);
-            if (kind == HIDDEN) continue;
-            f32x16 x = 0.f, dp = 0.f;
+        check(ROWS ? i + 1 : i - 1);
+        fetch_both(ROWS ? i + 2 : i);
+        const int cp = opaque(cplace), rp = opaque(rplace);
+        // (block -1 is the zeros)
+        const char* cbuf = s_k[0] + ((i - 1) & (NK - 1)) * TL::BYTES;
+        const char *kbuf = s_k[0] + ((i + 1) & (NK - 1)) * TL::BYTES, *vbuf = s_v[0] + (ROWS ? ((i + 1) & 1) * TL::BYTES : 0);
+        u32x4 ra[AHEAD ? 2 * TL::KS : 1];
+        if constexpr (AHEAD) {
 #pragma unroll
             for (int s = 0; s < TL::KS; ++s) {
-                x = P::mma(TL::rows_piece(s_k, u, s, lane), qf[s], x);
-                dp = P::mma(TL::rows_piece(s_v, u, s, lane), gf[s], dp);
+                ra[2 * s] = TL::rows_piece(kbuf, rp, s);
+                ra[2 * s + 1] = TL::rows_piece(vbuf, rp, s);
             }
-            float ds[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float th = 0.f;
-                const float p = prob<CAP>(x[i], c, ci, lse2, &th);
-                ds[i] = p * (dp[i] - del);
-                if (CAP) ds[i] *= 1.f - th * th;
-                if (kind == EDGE)
-                    ds[i] = visible(row, key0 + 32 * u + 8 * (i / 4) + 4 * hh + i % 4, A.window, A.sinks) ? ds[i] : 0.f;
-            }
-#pragma unroll
-            for (int s = 0; s < TL::US; ++s) {
-                const u32x4 pf = P::pack(ds + s * P::E);
-#pragma unroll
-                for (int db = 0; db < TL::DB; ++db) acc[db] = P::mma(TL::comps_piece(s_kc, db, u, s, lane), pf, acc[db]);
-            }
-            const unsigned marks = s_bad[t & 1][u];
-            if (edge && marks != 0u && spoiled_by<true>(marks, row, key0 + 32 * u, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
+            __builtin_amdgcn_sched_barrier(0);
         }
-    }
-    spoiled += other_half(spoiled);
+        u32x4 pn[TL::US];
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s) {
+            float ds[8];
+#pragma unroll
+            for (int j = 0; j < P::E; ++j) {
+                const float z = x[s * P::E + j];
+                ds[j] = __builtin_amdgcn_exp2f(fmaf(z, c, -lse2)) * (dx[s * P::E + j] - del);
+                if (CAP) ds[j] = z > -2.f ? ds[j] * (1.f - z * z) : 0.f;
+            }
+            pn[s] = P::pack(ds);
+            if constexpr (AHEAD) asm volatile("" : "+v"(pn[s]));
+        }
+        if constexpr (AHEAD) {
+            __builtin_amdgcn_sched_barrier(0);
+            x = 0.f;
+            dx = 0.f;
+#pragma unroll
+            for (int s = 0; s < TL::KS; ++s) {
+                x = P::mma(ra[2 * s], qf[s], x);
+                dx = P::mma(ra[AHEAD ? 2 * s + 1 : 0], gf[s], dx);
+            }
+        } else scores(min(i + 1, W.tiles - 1), x, dx);
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+            for (int db = 0; db < TL::DB; ++db) acc[db] = P::mma(TL::comps_piece(cbuf, cp, db, s), pf[s], acc[db]);
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s) pf[s] = pn[s];
+        __builtin_amdgcn_sched_barrier(0);
+        finish(key_at(i + 1));
+        if (i > 0) look(i - 1);
+    };
+    scores(0, x, dx);
+    finish(key_at(0));
+#pragma unroll 1
+    for (int i = 0; i < W.blocks; ++i) step(i);
+    dma_wait();
+    __syncthreads();
+    const int i = W.blocks - 1;
+    if constexpr (!ROWS) check(i);
+    if (row0 >= sq.len) return;
+#pragma unroll
+    for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+        for (int db = 0; db < TL::DB; ++db) acc[db] = P::mma(TL::comps_piece(s_k[0] + (i & (NK - 1)) * TL::BYTES, cplace, db, s), pf[s], acc[db]);
+    look(i);
+    spoiled = halves_sum(spoiled);
     store_row<T, D>(real ? dq + qoff : nullptr, acc, A.scale + spoiled, lane);
 }
 
-// FAR: the rows behind the window of 64 sinks, one query head and one chunk of rows per work-group; sums in 32 bits to `part`.
-// Otherwise the rows from a key tile's own to the end of its window, of every query head; to dk and dv, or, where far rows
-// follow, in 32 bits to `part`.
-template <typename T, int D, bool CAP, bool FAR>
-__global__ __launch_bounds__(WTHR, (dkv_waves<T, D>())) void window_dkv_kernel(WindowArgs A, FarPlan F, int tiles, const T* __restrict__ q,
-                                                                             const T* __restrict__ k, const T* __restrict__ v,
-                                                                             const float* __restrict__ lse, const T* __restrict__ dout,
-                                                                             const float* __restrict__ delta, float* __restrict__ part,
-                                                                             T* __restrict__ dk, T* __restrict__ dv)
+// P and dS of a lane's 16 pairs from its scores (tanh of them with a softcap) and dP, packed as operands.  ls, dl: the log-sum-exps (log2 units)
+// and deltas of the 16 rows, in LDS.  A pair that is hidden has a score of -inf (softcap: -1e30) and dP = 0.
+template <typename T, bool CAP>
+__device__ inline void probabilities(const f32x16& x, const f32x16& dp, float c, const float* ls, const float* dl, int hh, u32x4* pf, u32x4* df)
 {
-    constexpr int R = bwd_tile<T, D>();
+    typedef Piece<T> P;
+    constexpr int US = 16 / P::E;
+#pragma unroll
+    for (int s = 0; s < US; ++s) {
+        float p[8], ds[8];
+#pragma unroll
+        for (int m = 0; m < P::E / 4; ++m) {
+            const int at = 8 * (s * P::E / 4 + m) + 4 * hh;
+            const float4 l4 = *(const float4*)(ls + at), d4 = *(const float4*)(dl + at);
+            const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = s * P::E + 4 * m + j;
+                const float e = __builtin_amdgcn_exp2f(fmaf(x[i], c, -lv[j]));
+                p[4 * m + j] = e;
+                ds[4 * m + j] = e * (dp[i] - dv[j]);
+                if (CAP) ds[4 * m + j] = x[i] > -2.f ? ds[4 * m + j] * (1.f - x[i] * x[i]) : 0.f;
+            }
+        }
+        pf[s] = P::pack(p);
+        df[s] = P::pack(ds);
+    }
+}
+
+// The rows from a key tile's own to the end of its window, of every query head; to dk and dv, or, where far rows follow, in 32 bits to `part`.
+// Step i: S and dP of block i + 1, P and dS of block i, dV += dout^T P and dK += Q^T dS of block i - 1 (rows in two buffers, as in the
+// forward kernel: by rows ahead, by components behind).
+template <typename T, int D, bool CAP>
+__global__ __launch_bounds__(WTHR, (D * (int)sizeof(T) <= 128 ? 2 : 1)) void window_dkv_kernel(WindowArgs A, FarPlan F, int tiles, const T* __restrict__ q, const T* __restrict__ k,
+                                                           const T* __restrict__ v, const float* __restrict__ lse,
+                                                           const T* __restrict__ dout, const float* __restrict__ delta,
+                                                           float* __restrict__ part, T* __restrict__ dk, T* __restrict__ dv)
+{
+    constexpr int R = dkv_tile<T, D>(), U = R / 32;
     typedef Tile<T, D, R> TL;
     typedef Piece<T> P;
-    // the keys' and values' operands stay in registers where they fit; above 256 bytes a row they are read again from L1 for every block
-    constexpr bool KEEP = D * (int)sizeof(T) <= 256;
-    __shared__ __attribute__((aligned(16))) char s_q[TL::RBYTES];
-    __shared__ __attribute__((aligned(16))) char s_qc[TL::TBYTES];
-    __shared__ __attribute__((aligned(16))) char s_g[TL::RBYTES];
-    __shared__ __attribute__((aligned(16))) char s_gc[TL::TBYTES];
-    __shared__ __attribute__((aligned(16))) float s_lse[R], s_del[R];
-    __shared__ unsigned s_bad[2][2];
+    // the keys' and values' operands stay in registers where they fit; above 256 bytes a row they are read again from L1 for every block.
+    // Rows of 1024 bytes do not fit LDS often enough: by rows they are read from L1 too
+    constexpr bool KEEP = D * (int)sizeof(T) <= 256, ROWS = D * (int)sizeof(T) <= 512;
+    // tiles from before their scores to behind their sums
+    constexpr int NB = !ROWS ? 2 : U == 2 ? 3 : 4;
+    __shared__ __attribute__((aligned(256))) char s_q[NB][TL::BYTES], s_g[NB][TL::BYTES];
+    __shared__ __attribute__((aligned(16))) float s_lse[4][R], s_del[4][R];
+    __shared__ unsigned s_bad[4][2], s_lost[4][2];
     const int lane = threadIdx.x & 63, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int G = A.Hq / A.Hkv;
-    int b, hk, key0, h0, h1, from, to;                        // keys of the wavefront; heads; rows [from, to) of the walk
-    Sequence sq;
-    float* slot = nullptr;                                    // [2][KEYS or FAR_KEYS][D] of the work-group
-    int slot_row = 0;                                         // first key of the wavefront in it
-    if constexpr (FAR) {
-        const long long w = work_of((long long)A.B * A.Hkv * F.blocks * G * F.chunks);
-        if (w < 0) return;
-        const int chunk = (int)(w % F.chunks), g = (int)(w / F.chunks % G), blk = (int)(w / F.chunks / G % F.blocks);
-        hk = (int)(w / F.chunks / G / F.blocks % A.Hkv);
-        b = (int)(w / F.chunks / G / F.blocks / A.Hkv);
-        sq = sequence_of(A, b);
-        key0 = blk * FAR_KEYS + 32 * (wave >> 1);
-        h0 = hk * G + g;
-        h1 = h0 + 1;
-        from = max(chunk * F.chunk, far_start<R>(blk * FAR_KEYS / KEYS, A.window));
-        to = min((chunk + 1) * F.chunk, sq.len);
-        if (from >= to) return;
-        slot = part + F.off_far / sizeof(float) + ((size_t)w * 2 + (wave & 1)) * 2 * FAR_KEYS * D;
-        slot_row = 32 * (wave >> 1);
-    } else {
-        const long long w = work_of((long long)A.B * A.Hkv * tiles);
-        if (w < 0) return;
-        const int tile = (int)(w % tiles);
-        hk = (int)(w / tiles % A.Hkv);
-        b = (int)(w / tiles / A.Hkv);
-        sq = sequence_of(A, b);
-        if (tile * KEYS >= sq.len) return;
-        key0 = tile * KEYS + 32 * wave;
-        h0 = hk * G;
-        h1 = h0 + G;
-        from = tile * KEYS / R * R;
-        to = min(far_start<R>(tile, A.window), sq.len);
-        if (F.any && tile < F.near_tiles) {
-            slot = part + F.off_near / sizeof(float) + (((size_t)b * A.Hkv + hk) * F.near_tiles + tile) * 2 * KEYS * D;
-            slot_row = 32 * wave;
-        }
-    }
+    const long long w = work_of((long long)A.B * A.Hkv * tiles);
+    if (w < 0) return;
+    const int tile = (int)(w % tiles), hk = (int)(w / tiles % A.Hkv), b = (int)(w / tiles / A.Hkv);
+    const Sequence sq = sequence_of(A, b);
+    if (tile * KEYS >= sq.len) return;
+    const int tkey = tile * KEYS, key0 = tkey + 32 * wave;    // keys of the work-group, of the wavefront
+    const int from = tkey, to = min(far_start(tile, A.window), sq.len);
     const int key = key0 + (lane & 31);
     const bool real = key < sq.len;
     const long long koff = (long long)sq.tb * A.ks[0] + (long long)hk * A.ks[1] + (long long)(sq.first + (real ? key : sq.len - 1)) * A.ks[2];
@@ -258,123 +333,401 @@ __global__ __launch_bounds__(WTHR, (dkv_waves<T, D>())) void window_dkv_kernel(W
     for (int i = 0; i < TL::DB; ++i) ak[i] = av[i] = 0.f;
     const float c = CAP ? A.softcap * LOG2E : A.scale * LOG2E;
     const float ci = CAP ? A.scale / A.softcap : 0.f;
-    if (threadIdx.x < 4) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
 
-    const int per_head = (to - from + R - 1) / R, count = per_head * (h1 - h0);
-    Stage<T, D, R> st;
-    float nlse = 0.f, ndel = 0.f;
-    auto fetch = [&](int t) {
-        const int h = h0 + t / per_head, r0 = from + t % per_head * R;
-        st.load(q + (long long)sq.tb * A.qs[0] + (long long)h * A.qs[1] + (long long)sq.first * A.qs[2], A.qs[2],
-                dout + (long long)sq.tb * A.os[0] + (long long)h * A.os[1] + (long long)sq.first * A.os[2], A.os[2], r0, to);
-        if (threadIdx.x < R) {
-            const int r = r0 + threadIdx.x;
-            const long long li = ((long long)sq.tb * A.Hq + h) * A.n + sq.first + r;
-            nlse = r < to ? lse[li] * LOG2E : INFINITY;       // a row that is not there has probabilities of zero
-            ndel = r < to ? delta[li] : 0.f;
+    // the walk: tiles of R rows, head after head, th of each head (rows behind `to` in the last one are hidden)
+    const int th = (to - from + R - 1) / R, ntiles = th * G;
+    // a tile of the walk: head, first row (from + j R), and where its rows and sums lie
+    struct Cursor {
+        int t, j, row;
+        const T *q, *g;
+        long long sums;
+    };
+    const long long qhead = A.qs[1], ghead = A.os[1], qstep = (long long)R * A.qs[2], gstep = (long long)R * A.os[2];
+    Cursor start;
+    start.t = start.j = 0;
+    start.row = from;
+    start.q = q + (long long)sq.tb * A.qs[0] + (long long)hk * G * qhead + (long long)(sq.first + from) * A.qs[2];
+    start.g = dout + (long long)sq.tb * A.os[0] + (long long)hk * G * ghead + (long long)(sq.first + from) * A.os[2];
+    start.sums = ((long long)sq.tb * A.Hq + hk * G) * A.n + sq.first + from;
+    auto advance = [&](Cursor& c) WINDOW_INLINE {              // (behind the last tile it stays there)
+        if (c.t + 1 >= ntiles) return;
+        ++c.t;
+        if (++c.j < th) {
+            c.row += R;
+            c.q += qstep;
+            c.g += gstep;
+            c.sums += R;
+        } else {
+            const int back = th - 1;
+            c.j = 0;
+            c.row = from;
+            c.q += qhead - back * qstep;
+            c.g += ghead - back * gstep;
+            c.sums += A.n - (long long)back * R;
         }
     };
-    fetch(0);
-    for (int t = 0; t < count; ++t) {
-        const int row0 = from + t % per_head * R;
-        const bool edge = FAR ? true : row0 < key0 - 32 * wave + KEYS || row0 + R - 1 - (key0 - 32 * wave) >= A.window;
-        __syncthreads();
-        if (edge) st.take_out_not_finite(s_bad[t & 1]);
-        if (threadIdx.x < 2) s_bad[(t + 1) & 1][threadIdx.x] = 0u;
-        st.store(s_q, s_qc, s_g, s_gc);
-        if (threadIdx.x < R) { s_lse[threadIdx.x] = nlse; s_del[threadIdx.x] = ndel; }
-        __syncthreads();
-        if (t + 1 < count) fetch(t + 1);
-        // far: the two wavefronts of a block of keys take the blocks of rows in turn
-        const int u0 = FAR && R == 64 ? wave & 1 : 0, u1 = FAR ? (R == 64 ? u0 + 1 : 1 - ((t ^ wave) & 1)) : R / 32;
-#pragma unroll 1
-        for (int u = u0; u < u1; ++u) {
-            const int r0 = row0 + 32 * u;
-            const Block kind = block_kind(r0, key0, A.window, A.sinks);
-            if (kind == HIDDEN) continue;
-            f32x16 x = 0.f, dp = 0.f;
-#pragma unroll
-            for (int s = 0; s < TL::KS; ++s) {
-                const u32x4 kk = KEEP ? kf[KEEP ? s : 0] : load_piece(k + koff, 2 * s + hh);
-                const u32x4 vv = KEEP ? vf[KEEP ? s : 0] : load_piece(v + koff, 2 * s + hh);
-                x = P::mma(TL::rows_piece(s_q, u, s, lane), kk, x);
-                dp = P::mma(TL::rows_piece(s_g, u, s, lane), vv, dp);
+    const int qpitch = (int)(A.qs[2] * (long long)sizeof(T)), gpitch = (int)(A.os[2] * (long long)sizeof(T));
+    Dma<T, D, R, 4> qdma, gdma;
+    qdma.init(wave, lane, qpitch);
+    gdma.init(wave, lane, gpitch);
+    float nlse = 0.f, ndel = 0.f;
+    Cursor crows = start, csums = start;                      // the next tiles to be fetched
+    int tsums = 0;                                            // and to be put (running on behind the last one)
+    int brows = 0;                                            // buffer of the next rows
+    auto edge_row = [&](int row) WINDOW_INLINE { return row < tkey + KEYS || row + R - 1 - tkey >= A.window; };
+    auto next_buffer = [&](int b) WINDOW_INLINE { return b + 1 == NB ? 0 : b + 1; };
+    auto fetch_rows = [&]() WINDOW_INLINE {
+        qdma.load(crows.q, qpitch, to - crows.row, s_q[0] + brows * TL::BYTES, wave, lane);
+        gdma.load(crows.g, gpitch, to - crows.row, s_g[0] + brows * TL::BYTES, wave, lane);
+        brows = next_buffer(brows);
+        advance(crows);
+    };
+    // the rows of tile t (first row `row`, in buffer b) have landed and are about to be met
+    auto check = [&](int t, int row, int b) WINDOW_INLINE {
+        if (threadIdx.x < 2) s_bad[(t + 1) & 3][threadIdx.x] = 0u;
+        if (t >= 0 && t < ntiles && edge_row(row)) {
+            scrub<T, D, R>(s_q[0] + b * TL::BYTES, s_bad[t & 3]);
+            scrub<T, D, R>(s_g[0] + b * TL::BYTES, s_bad[t & 3]);
+            __syncthreads();
+        }
+    };
+    bool sums_edge = false;
+    int sums_row = 0;
+    auto fetch_sums = [&]() WINDOW_INLINE {
+        sums_edge = edge_row(csums.row);
+        sums_row = csums.row;
+        if (wave == 0 && lane < R) {
+            const bool there = csums.row + lane < to;
+            nlse = there ? lse[csums.sums + lane] * LOG2E : INFINITY;   // a row that is not there has probabilities of zero
+            ndel = there ? delta[csums.sums + lane] : 0.f;
+        }
+        advance(csums);
+    };
+    // (a row whose sums are not finite would spoil keys that do not see it: in a tile with hidden pairs it is taken out and marked)
+    auto put_sums = [&]() WINDOW_INLINE {
+        if (wave == 0) {
+            bool lost = false;
+            if (sums_edge) {
+                lost = lane < R && sums_row + lane < to && !(fabsf(nlse) < INFINITY && fabsf(ndel) < INFINITY);
+                nlse = lost ? INFINITY : nlse;
+                ndel = lost ? 0.f : ndel;
             }
-            float p[16], ds[16];
+            const unsigned long long all = __ballot(lost);
+            if (lane == 0) { s_lost[tsums & 3][0] = (unsigned)all; s_lost[tsums & 3][1] = (unsigned)(all >> 32); }
+            if (lane < R) { s_lse[tsums & 3][lane] = nlse; s_del[tsums & 3][lane] = ndel; }
+        }
+        ++tsums;
+    };
+    if (threadIdx.x < 8) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
+    for (int i = threadIdx.x; i < TL::BYTES / 16; i += WTHR) {          // (met by weights of zero before they are filled)
+        *(u32x4*)(s_q[NB - 1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};
+        *(u32x4*)(s_g[NB - 1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};
+    }
+    if constexpr (ROWS) {
+        fetch_rows();
+        fetch_rows();
+    }
+    fetch_sums();
+    put_sums();
+    fetch_sums();
+    put_sums();
+    fetch_sums();
+    dma_wait();
+    __syncthreads();
+    if constexpr (ROWS) check(0, from, 0);
+
+    const int rplace = TL::rows_place(lane), cplace = TL::comps_place(lane);
+    f32x16 x, dx;
+    u32x4 pf[TL::US], df[TL::US];
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const float4 l4 = *(const float4*)(s_lse + 32 * u + 8 * m + 4 * hh), d4 = *(const float4*)(s_del + 32 * u + 8 * m + 4 * hh);
-                const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
+    for (int s = 0; s < TL::US; ++s) pf[s] = df[s] = 0u;
+    // operands of the scores' products from LDS, or from memory (rows row0 .. of the head at qr, gr)
+    auto row_piece = [&](const char* buf, const T* base, long long stride, int row0, int rp, int s) WINDOW_INLINE {
+        return ROWS ? TL::rows_piece(buf, rp, s) : load_piece(base + (long long)min(lane & 31, to - 1 - row0) * stride, 2 * s + hh);
+    };
+    auto key_piece = [&](const u32x4* kept, const T* base, int s) WINDOW_INLINE { return KEEP ? kept[KEEP ? s : 0] : load_piece(base + koff, 2 * s + hh); };
+    const int open0 = key0 + 31, open1 = key0 - 32 + A.window;           // blocks from row open0 to open1 hide nothing
+    auto finish = [&](int row0) WINDOW_INLINE {
+        if (CAP) tanh_scores<T>(x, ci);
+        if (row0 >= open0 && row0 <= open1 && row0 + 32 <= to) return;
+        const int row = opaque(row0 + 4 * hh);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int i = 4 * m + j;
-                    float th = 0.f;
-                    p[i] = prob<CAP>(x[i], c, ci, ls[j], &th);
-                    ds[i] = p[i] * (dp[i] - dl[j]);
-                    if (CAP) ds[i] *= 1.f - th * th;
-                    if (kind == EDGE) {
-                        const int row = r0 + 8 * m + 4 * hh + j;
-                        const bool seen = row < to && visible(row, key, A.window, A.sinks);
-                        p[i] = seen ? p[i] : 0.f;
-                        ds[i] = seen ? ds[i] : 0.f;
-                    }
-                }
-            }
+        for (int i = 0; i < 16; ++i) {
+            const int r = row + 8 * (i / 4) + i % 4;
+            const bool seen = (bool)((int)(r < to) & (int)visible(r, key, A.window, A.sinks));
+            x[i] = seen ? x[i] : CAP ? -1e30f : -INFINITY;
+            dx[i] = seen ? dx[i] : 0.f;
+        }
+    };
+    auto look = [&](int t, int u, int row0) WINDOW_INLINE {
+        if (!edge_row(row0 - 32 * u)) return;
+        const unsigned marks = s_bad[t & 3][u] | s_lost[t & 3][u];
+        if (marks != 0u && spoiled_by<false>(marks, key, row0, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
+    };
+    {
+        const int rp = opaque(rplace);
+        x = 0.f;
+        dx = 0.f;
 #pragma unroll
-            for (int s = 0; s < TL::US; ++s) {
-                const u32x4 pf = P::pack(p + s * P::E), df = P::pack(ds + s * P::E);
-#pragma unroll
-                for (int db = 0; db < TL::DB; ++db) {
-                    av[db] = P::mma(TL::comps_piece(s_gc, db, u, s, lane), pf, av[db]);
-                    ak[db] = P::mma(TL::comps_piece(s_qc, db, u, s, lane), df, ak[db]);
-                }
-            }
-            const unsigned marks = s_bad[t & 1][u];
-            if (edge && marks != 0u && spoiled_by<false>(marks, key, r0, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
+        for (int s = 0; s < TL::KS; ++s) {
+            x = P::mma(row_piece(s_q[0], start.q, A.qs[2], from, rp, s), key_piece(kf, k, s), x);
+            dx = P::mma(row_piece(s_g[0], start.g, A.os[2], from, rp, s), key_piece(vf, v, s), dx);
         }
     }
-    spoiled += other_half(spoiled);
-    if (slot) {
-        // (what is at and behind the sinks of a far slot, or behind the sequence, is not read)
-        const bool keep = real && (!FAR || key < A.sinks);
-        float* at = slot + (size_t)(slot_row + (lane & 31)) * D;
-        store_row<float, D>(keep ? at : nullptr, ak, A.scale + spoiled, lane);
-        store_row<float, D>(keep ? at + (size_t)(FAR ? FAR_KEYS : KEYS) * D : nullptr, av, 1.f + spoiled, lane);
+    finish(from);
+    Cursor here = start;
+    int tv = 0, uv = 0, rowv = -1, bv = NB - 1, bh = 0, t = 0;           // the block before: tile, place, row, buffer (none yet: the zeros); this one's buffer
+#pragma unroll 1
+    for (; t < ntiles; ++t) {
+        Cursor ahead = here;
+        advance(ahead);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u == U - 1) {
+                // the last step of tile t: the next rows on their way
+                dma_wait();
+                __syncthreads();
+                if constexpr (ROWS) check(t + 1, ahead.row, next_buffer(bh));
+                else check(t - 1, rowv, bv);
+                put_sums();
+                fetch_rows();
+                fetch_sums();
+            }
+            const bool same = u + 1 < U;
+            const int rowk = same ? here.row + 32 * (u + 1) : ahead.row, bk = same ? bh : next_buffer(bh);
+            const char *qk = s_q[0] + bk * TL::BYTES + (same ? TL::BLOCK * (u + 1) : 0), *gk = s_g[0] + bk * TL::BYTES + (same ? TL::BLOCK * (u + 1) : 0);
+            const char *qv = s_q[0] + bv * TL::BYTES + TL::BLOCK * uv, *gv = s_g[0] + bv * TL::BYTES + TL::BLOCK * uv;
+            const int rp = opaque(rplace), cp = opaque(cplace);
+            // reads, then the vector work, then the products (KEEP: all operands wait in registers)
+            u32x4 ca[KEEP ? 2 * TL::US * TL::DB : 1], ra[KEEP ? 2 * TL::KS : 1];
+            if constexpr (KEEP) {
+#pragma unroll
+                for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+                    for (int db = 0; db < TL::DB; ++db) {
+                        ca[2 * (s * TL::DB + db)] = TL::comps_piece(gv, cp, db, s);
+                        ca[2 * (s * TL::DB + db) + 1] = TL::comps_piece(qv, cp, db, s);
+                    }
+#pragma unroll
+                for (int s = 0; s < TL::KS; ++s) {
+                    ra[2 * s] = TL::rows_piece(qk, rp, s);
+                    ra[2 * s + 1] = TL::rows_piece(gk, rp, s);
+                }
+            }
+            u32x4 pn[TL::US], dn[TL::US];
+            probabilities<T, CAP>(x, dx, c, &s_lse[t & 3][32 * u], &s_del[t & 3][32 * u], hh, pn, dn);
+#pragma unroll
+            for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+                for (int db = 0; db < TL::DB; ++db) {
+                    const int at = KEEP ? 2 * (s * TL::DB + db) : 0;
+                    av[db] = P::mma(KEEP ? ca[at] : TL::comps_piece(gv, cp, db, s), pf[s], av[db]);
+                    ak[db] = P::mma(KEEP ? ca[KEEP ? at + 1 : 0] : TL::comps_piece(qv, cp, db, s), df[s], ak[db]);
+                }
+            x = 0.f;
+            dx = 0.f;
+#pragma unroll
+            for (int s = 0; s < TL::KS; ++s) {
+                const T *qr = (same ? here.q : ahead.q) + (same ? 32 * (u + 1) * A.qs[2] : 0), *gr = (same ? here.g : ahead.g) + (same ? 32 * (u + 1) * A.os[2] : 0);
+                x = P::mma(KEEP ? ra[KEEP ? 2 * s : 0] : row_piece(qk, qr, A.qs[2], rowk, rp, s), key_piece(kf, k, s), x);
+                dx = P::mma(KEEP ? ra[KEEP ? 2 * s + 1 : 0] : row_piece(gk, gr, A.os[2], rowk, rp, s), key_piece(vf, v, s), dx);
+            }
+            if constexpr (KEEP) {
+#pragma unroll
+                for (int s = 0; s < TL::US; ++s) asm volatile("" : "+v"(pn[s]), "+v"(dn[s]));
+                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+                for (int j = 0; j < 2 * TL::KS + 2 * TL::US * TL::DB; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int s = 0; s < TL::US; ++s) { pf[s] = pn[s]; df[s] = dn[s]; }
+            finish(rowk);
+            if (rowv >= 0) look(tv, uv, rowv);
+            tv = t;
+            uv = u;
+            rowv = here.row + 32 * u;
+            bv = bh;
+        }
+        here = ahead;
+        bh = next_buffer(bh);
+    }
+    dma_wait();
+    __syncthreads();
+    if constexpr (!ROWS) check(tv, rowv, bv);
+    {
+        const int cp = opaque(cplace);
+        const char *qv = s_q[0] + bv * TL::BYTES + TL::BLOCK * uv, *gv = s_g[0] + bv * TL::BYTES + TL::BLOCK * uv;
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+            for (int db = 0; db < TL::DB; ++db) {
+                av[db] = P::mma(TL::comps_piece(gv, cp, db, s), pf[s], av[db]);
+                ak[db] = P::mma(TL::comps_piece(qv, cp, db, s), df[s], ak[db]);
+            }
+    }
+    look(tv, uv, rowv);
+    spoiled = halves_sum(spoiled);
+    if (F.any && tile < F.near_tiles) {
+        float* at = part + F.off_near / sizeof(float) + (((size_t)b * A.Hkv + hk) * F.near_tiles + tile) * 2 * KEYS * D + (size_t)(key - tkey) * D;
+        store_row<float, D>(real ? at : nullptr, ak, A.scale + spoiled, lane);
+        store_row<float, D>(real ? at + (size_t)KEYS * D : nullptr, av, 1.f + spoiled, lane);
     } else {
         store_row<T, D>(real ? dk + koff : nullptr, ak, A.scale + spoiled, lane);
         store_row<T, D>(real ? dv + koff : nullptr, av, 1.f + spoiled, lane);
     }
 }
 
-// dk and dv of the key tiles that hold sinks: the owner's sums, then the far chunks' head by head and chunk by chunk.
-// One work-group per (b, KV head, key), a thread per component of dk, then of dv.
-template <typename T, int R>
+// The rows behind the window of 32 sinks, one query head and one chunk of rows per work-group: its wavefronts take blocks of 32 rows in turn, each
+// by itself, through LDS of its own, and join their sums in LDS, in order.
+template <typename T, int D> constexpr int far_waves() { return D > 128 ? 2 : 4; }     // (what fits LDS)
+template <typename T, int D, bool CAP>
+__global__ __launch_bounds__((64 * far_waves<T, D>()), 1) void window_far_kernel(WindowArgs A, FarPlan F, const T* __restrict__ q,
+                                                                             const T* __restrict__ k, const T* __restrict__ v,
+                                                                             const float* __restrict__ lse, const T* __restrict__ dout,
+                                                                             const float* __restrict__ delta, float* __restrict__ part)
+{
+    typedef Tile<T, D, 32> TL;
+    typedef Piece<T> P;
+    constexpr int WAVES = far_waves<T, D>();
+    constexpr bool KEEP = D * (int)sizeof(T) <= 256;
+    constexpr int PER = 2 * TL::BYTES + 256;                  // of a wavefront: Q and dout, lse and delta of the rows
+    constexpr int JOIN = 2 * FAR_KEYS * (D + 4) * 4;
+    __shared__ __attribute__((aligned(256))) char smem[WAVES * PER > JOIN ? WAVES * PER : JOIN];
+    const int lane = threadIdx.x & 63, hh = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int G = A.Hq / A.Hkv;
+    const long long w = work_of((long long)A.B * A.Hkv * F.blocks * G * F.chunks);
+    if (w < 0) return;
+    const int chunk = (int)(w % F.chunks), g = (int)(w / F.chunks % G), blk = (int)(w / F.chunks / G % F.blocks);
+    const int hk = (int)(w / F.chunks / G / F.blocks % A.Hkv), b = (int)(w / F.chunks / G / F.blocks / A.Hkv);
+    const Sequence sq = sequence_of(A, b);
+    const int from = max(chunk * F.chunk, far_start(blk * FAR_KEYS / KEYS, A.window)), to = min((chunk + 1) * F.chunk, sq.len);
+    if (from >= to) return;
+    const int h = hk * G + g, key = blk * FAR_KEYS + col;
+    const bool sink = key < A.sinks;                          // (from > every key of the block: a sink is seen by all these rows)
+    const long long koff = (long long)sq.tb * A.ks[0] + (long long)hk * A.ks[1] + (long long)(sq.first + (sink ? key : A.sinks - 1)) * A.ks[2];
+    const T* qb = q + (long long)sq.tb * A.qs[0] + (long long)h * A.qs[1] + (long long)sq.first * A.qs[2];
+    const T* gb = dout + (long long)sq.tb * A.os[0] + (long long)h * A.os[1] + (long long)sq.first * A.os[2];
+    const long long lb = ((long long)sq.tb * A.Hq + h) * A.n + sq.first;
+    char *qt = smem + wave * PER, *gt = qt + TL::BYTES;
+    float *ls = (float*)(gt + TL::BYTES), *dl = ls + 32;
+    const int qpitch = (int)(A.qs[2] * (long long)sizeof(T)), gpitch = (int)(A.os[2] * (long long)sizeof(T));
+    Dma<T, D, 32, 1> qdma, gdma;
+    qdma.init(0, lane, qpitch);
+    gdma.init(0, lane, gpitch);
+
+    u32x4 kf[KEEP ? TL::KS : 1], vf[KEEP ? TL::KS : 1];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int s = 0; s < TL::KS; ++s) {
+            kf[s] = load_piece(k + koff, 2 * s + hh);
+            vf[s] = load_piece(v + koff, 2 * s + hh);
+        }
+    }
+    f32x16 ak[TL::DB], av[TL::DB];
+#pragma unroll
+    for (int i = 0; i < TL::DB; ++i) ak[i] = av[i] = 0.f;
+    const float c = CAP ? A.softcap * LOG2E : A.scale * LOG2E;
+    const float ci = CAP ? A.scale / A.softcap : 0.f;
+    const int rplace = TL::rows_place(lane), cplace = TL::comps_place(lane);
+    for (int row0 = from + 32 * wave; row0 < to; row0 += 32 * WAVES) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the block before has been read
+        qdma.load(qb + (long long)row0 * A.qs[2], qpitch, to - row0, qt, 0, lane);
+        gdma.load(gb + (long long)row0 * A.os[2], gpitch, to - row0, gt, 0, lane);
+        const int r = min(row0 + col, to - 1);
+        const float l1 = row0 + col < to ? lse[lb + r] * LOG2E : INFINITY, d1 = row0 + col < to ? delta[lb + r] : 0.f;
+        if (hh == 0) { ls[col] = l1; dl[col] = d1; }
+        dma_wait();
+        own_fence();
+        f32x16 x = 0.f, dx = 0.f;
+#pragma unroll
+        for (int s = 0; s < TL::KS; ++s) {
+            const u32x4 kk = KEEP ? kf[KEEP ? s : 0] : load_piece(k + koff, 2 * s + hh);
+            const u32x4 vv = KEEP ? vf[KEEP ? s : 0] : load_piece(v + koff, 2 * s + hh);
+            x = P::mma(TL::rows_piece(qt, rplace, s), kk, x);
+            dx = P::mma(TL::rows_piece(gt, rplace, s), vv, dx);
+        }
+        if (CAP) tanh_scores<T>(x, ci);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool there = row0 + 8 * (i / 4) + 4 * hh + i % 4 < to;
+            x[i] = there ? x[i] : CAP ? -1e30f : -INFINITY;
+            dx[i] = there ? dx[i] : 0.f;
+        }
+        u32x4 pf[TL::US], df[TL::US];
+        probabilities<T, CAP>(x, dx, c, ls, dl, hh, pf, df);
+#pragma unroll
+        for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+            for (int db = 0; db < TL::DB; ++db) {
+                av[db] = P::mma(TL::comps_piece(gt, cplace, db, s), pf[s], av[db]);
+                ak[db] = P::mma(TL::comps_piece(qt, cplace, db, s), df[s], ak[db]);
+            }
+    }
+    float* sum = (float*)smem;                                // [2][32][D + 4]
+    for (int turn = 0; turn < WAVES; ++turn) {
+        __syncthreads();
+        if (wave != turn) continue;
+#pragma unroll
+        for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int comp = 32 * db + 8 * (i / 4) + 4 * hh + i % 4;
+                if (comp >= D) continue;
+                float *a = sum + col * (D + 4) + comp, *z = a + FAR_KEYS * (D + 4);
+                *a = (turn ? *a : 0.f) + ak[db][i] * A.scale;
+                *z = (turn ? *z : 0.f) + av[db][i];
+            }
+    }
+    __syncthreads();
+    float* slot = part + F.off_far / sizeof(float) + (size_t)w * 2 * FAR_KEYS * D;
+    const int sinks = min(FAR_KEYS, A.sinks - blk * FAR_KEYS);          // (what lies behind them is not read)
+    for (int i = threadIdx.x; i < 2 * sinks * D; i += 64 * WAVES) {
+        const int which = i / (sinks * D), j = i % (sinks * D);
+        slot[(size_t)which * FAR_KEYS * D + j] = sum[(which * FAR_KEYS + j / D) * (D + 4) + j % D];
+    }
+}
+
+// dk and dv of the key tiles that hold sinks: the owner's sums, then the far chunks' head by head and chunk by chunk (in four shares, joined in
+// order).  One work-group per (b, KV head, key), 64 components of dk or dv at a time.
+template <typename T>
 __global__ __launch_bounds__(WTHR) void window_join_kernel(WindowArgs A, FarPlan F, const float* __restrict__ part, T* __restrict__ dk,
                                                           T* __restrict__ dv)
 {
+    __shared__ float s_sum[4][64];
     const int keys = F.near_tiles * KEYS;
     const int key = (int)(blockIdx.x % keys), hk = (int)(blockIdx.x / keys % A.Hkv), b = (int)(blockIdx.x / keys / A.Hkv);
     const Sequence sq = sequence_of(A, b);
     if (key >= sq.len) return;
-    const int G = A.Hq / A.Hkv, d = A.d, blk = key / FAR_KEYS;
-    const int start = far_start<R>(key / KEYS, A.window);
+    const int G = A.Hq / A.Hkv, d = A.d, share = threadIdx.x >> 6, c0 = threadIdx.x & 63;
+    const int start = far_start(key / KEYS, A.window);
+    // far chunks that have rows: from the one that holds `start` on
+    const int c1 = start / F.chunk, n = key < A.sinks && start < sq.len ? (sq.len - 1) / F.chunk - c1 + 1 : 0;
     const float* near = part + F.off_near / sizeof(float) + (((size_t)b * A.Hkv + hk) * F.near_tiles + key / KEYS) * 2 * KEYS * d;
-    const float* far = part + F.off_far / sizeof(float) + (((size_t)b * A.Hkv + hk) * F.blocks + blk) * G * F.chunks * 2 * 2 * FAR_KEYS * d;
+    const float* far = part + F.off_far / sizeof(float) + ((((size_t)b * A.Hkv + hk) * F.blocks + key / FAR_KEYS) * G * F.chunks * 2 * FAR_KEYS +
+                                                          key % FAR_KEYS) * d;
     const long long off = (long long)sq.tb * A.ks[0] + (long long)hk * A.ks[1] + (long long)(sq.first + key) * A.ks[2];
-    for (int i = threadIdx.x; i < 2 * d; i += WTHR) {
-        const int which = i >= d, comp = which ? i - d : i;
-        float sum = near[((size_t)which * KEYS + key % KEYS) * d + comp];
-        if (key < A.sinks)
-            for (int g = 0; g < G; ++g)
-                for (int c = 0; c < F.chunks; ++c) {
-                    if (max(c * F.chunk, start) >= min((c + 1) * F.chunk, sq.len)) continue;
-                    for (int half = 0; half < 2; ++half)
-                        sum += far[((((size_t)g * F.chunks + c) * 2 + half) * 2 + which) * FAR_KEYS * d + (size_t)(key % FAR_KEYS) * d + comp];
-                }
-        T* to = (which ? dv : dk) + off + comp;
-        const float x[8] = {sum, sum, sum, sum, sum, sum, sum, sum};
-        const u32x4 p = Piece<T>::pack(x);
-        __builtin_memcpy(to, &p, sizeof(T));
+    for (int i = 0; i < 2 * d; i += 64) {
+        const int which = i + c0 >= d, comp = which ? i + c0 - d : i + c0;
+        const bool there = i + c0 < 2 * d;
+        float sum = there && share == 0 ? near[((size_t)which * KEYS + key % KEYS) * d + comp] : 0.f;
+#pragma unroll 4
+        for (int j = share * G * n / 4; there && j < (share + 1) * G * n / 4; ++j)
+            sum += far[((size_t)(j / n) * F.chunks + c1 + j % n) * 2 * FAR_KEYS * d + (size_t)which * FAR_KEYS * d + comp];
+        s_sum[share][c0] = sum;
+        __syncthreads();
+        if (share == 0 && there) {
+            sum = (s_sum[0][c0] + s_sum[1][c0]) + (s_sum[2][c0] + s_sum[3][c0]);
+            const float y[8] = {sum, sum, sum, sum, sum, sum, sum, sum};
+            const u32x4 p = Piece<T>::pack(y);
+            __builtin_memcpy((which ? dv : dk) + off + comp, &p, sizeof(T));
+        }
+        __syncthreads();
     }
 }
 
@@ -384,25 +737,23 @@ hipError_t launch_cap(const WindowArgs& A, const void* q_, const void* k_, const
 {
     const T *q = (const T*)q_, *k = (const T*)k_, *v = (const T*)v_, *out = (const T*)out_, *dout = (const T*)dout_;
     T *dk = (T*)dk_, *dv = (T*)dv_;
-    constexpr int R = bwd_tile<T, D>();
     const FarPlan F = far_plan(A);
     float *delta = (float*)ws, *part = (float*)ws;
-    const int G = A.Hq / A.Hkv, heads = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1, rows = 32 * (4 / heads);
-    const int tiles = (A.span_max + rows - 1) / rows, ktiles = (A.span_max + KEYS - 1) / KEYS;
-    const long long g1 = work_groups((long long)A.B * A.Hkv * tiles * (G / heads)), g2 = work_groups((long long)A.B * A.Hkv * ktiles);
+    const int G = A.Hq / A.Hkv, blocks = (A.span_max + 31) / 32, ktiles = (A.span_max + KEYS - 1) / KEYS;
+    const long long g1 = work_groups((long long)A.B * A.Hkv * ((blocks * G + 3) / 4)), g2 = work_groups((long long)A.B * A.Hkv * ktiles);
     const long long g3 = F.any ? work_groups((long long)A.B * A.Hkv * F.blocks * G * F.chunks) : 0;
     const long long g4 = F.any ? (long long)A.B * A.Hkv * F.near_tiles * KEYS : 0;
     if (std::max(std::max(g1, g2), std::max(g3, g4)) > 0x7fffffffll) return hipErrorInvalidConfiguration;
-    window_dq_kernel<T, D, CAP><<<(unsigned)g1, WTHR, 0, st>>>(A, tiles, heads, q, k, v, out, lse, dout, delta, (T*)dq);
+    window_dq_kernel<T, D, CAP><<<(unsigned)g1, WTHR, 0, st>>>(A, blocks, q, k, v, out, lse, dout, delta, (T*)dq);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    window_dkv_kernel<T, D, CAP, false><<<(unsigned)g2, WTHR, 0, st>>>(A, F, ktiles, q, k, v, lse, dout, delta, part, dk, dv);
+    window_dkv_kernel<T, D, CAP><<<(unsigned)g2, WTHR, 0, st>>>(A, F, ktiles, q, k, v, lse, dout, delta, part, dk, dv);
     e = hipGetLastError();
     if (e != hipSuccess || !F.any) return e;
-    window_dkv_kernel<T, D, CAP, true><<<(unsigned)g3, WTHR, 0, st>>>(A, F, ktiles, q, k, v, lse, dout, delta, part, dk, dv);
+    window_far_kernel<T, D, CAP><<<(unsigned)g3, 64 * far_waves<T, D>(), 0, st>>>(A, F, q, k, v, lse, dout, delta, part);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    window_join_kernel<T, R><<<(unsigned)g4, WTHR, 0, st>>>(A, F, part, dk, dv);
+    window_join_kernel<T><<<(unsigned)g4, WTHR, 0, st>>>(A, F, part, dk, dv);
     return hipGetLastError();
 }
 template <typename T, int D, typename... X>

@@ -62,11 +62,10 @@ __global__ __launch_bounds__(WTHR, (dec_waves<T, D>())) void window_step_kernel(
     typedef Tile<T, D, 32> TL;
     typedef Piece<T> P;
     constexpr bool AHEAD = D * (int)sizeof(T) <= 256;         // loads of the next keys during the products of these (registers)
-    constexpr int VB = TL::BLOCKS / 64;                       // 4-row blocks of V for a lane
-    constexpr int VBX = (TL::BLOCKS + 63) / 64;
+    constexpr int VBX = TL::BYTES / 1024;                     // loads of a round of V
     constexpr int JOIN = COLS * (D + 4) * 4;
-    constexpr int SMEM = 4 * TL::TBYTES > JOIN ? 4 * TL::TBYTES : JOIN;
-    __shared__ __attribute__((aligned(16))) char smem[SMEM];
+    constexpr int SMEM = 4 * TL::BYTES > JOIN ? 4 * TL::BYTES : JOIN;
+    __shared__ __attribute__((aligned(256))) char smem[SMEM];
     __shared__ float s_m[4][COLS], s_l[4][COLS];
     const int lane = threadIdx.x & 63, hh = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -110,45 +109,22 @@ __global__ __launch_bounds__(WTHR, (dec_waves<T, D>())) void window_step_kernel(
         }
         return cache + (size_t)row * D;
     };
-    u32x4 kf[AHEAD ? TL::KS : 1], vr[AHEAD ? VBX : 1][4];
+    u32x4 kf[AHEAD ? TL::KS : 1], vr[AHEAD ? VBX : 1];
     auto load_k = [&](int u0) {
         const T* r = row_of(min(u0 + col, S.count - 1), kcb, knb);
 #pragma unroll
         for (int s = 0; s < (AHEAD ? TL::KS : 0); ++s) kf[s] = load_piece(r, 2 * s + hh);
     };
+    const int cplace = TL::comps_place(lane);
+    char* mine = smem + wave * TL::BYTES;
+    // V: row r of the round to its place, 16 bytes a lane
     auto load_v = [&](int u0, int i, u32x4* x) {
-        const int id = lane + 64 * i, g = id % 8, piece = id / 8;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            u32x4 y = {0u, 0u, 0u, 0u};
-            if (piece < TL::PIECES && u0 + 4 * g + j < S.count) y = load_piece(row_of(u0 + 4 * g + j, vcb, vnb), piece);
-            x[j] = y;
-        }
+        const int id = 64 * i + lane, r = id / (TL::RPITCH / 16), piece = (id % (TL::RPITCH / 16)) ^ TL::turn_of_row(r);
+        u32x4 y = {0u, 0u, 0u, 0u};
+        if (u0 + r < S.count && piece < TL::PIECES) y = load_piece(row_of(u0 + r, vcb, vnb), piece);
+        *x = y;
     };
-    char* mine = smem + wave * TL::TBYTES;
-    auto store_v = [&](int i, const u32x4* x) {
-        const int id = lane + 64 * i, g = id % 8, piece = id / 8;
-        if (VB != VBX && piece >= TL::PIECES) return;
-        char* at = mine + piece * TL::E * TL::TPITCH + TL::slot_of_rows(g) * TL::ES;
-        if constexpr (TL::ES == 4) {
-#pragma unroll
-            for (int cc = 0; cc < 4; ++cc) {
-                const u32x4 y = {x[0][cc], x[1][cc], x[2][cc], x[3][cc]};
-                *(u32x4*)(at + cc * TL::TPITCH) = y;
-            }
-        } else {
-#pragma unroll
-            for (int cc = 0; cc < 4; ++cc) {
-                uint2 lo, hi;
-                lo.x = __builtin_amdgcn_perm(x[1][cc], x[0][cc], 0x05040100u);
-                lo.y = __builtin_amdgcn_perm(x[3][cc], x[2][cc], 0x05040100u);
-                hi.x = __builtin_amdgcn_perm(x[1][cc], x[0][cc], 0x07060302u);
-                hi.y = __builtin_amdgcn_perm(x[3][cc], x[2][cc], 0x07060302u);
-                *(uint2*)(at + 2 * cc * TL::TPITCH) = lo;
-                *(uint2*)(at + (2 * cc + 1) * TL::TPITCH) = hi;
-            }
-        }
-    };
+    auto store_v = [&](int i, const u32x4* x) { *(u32x4*)(mine + 16 * (64 * i + lane)) = *x; };
 
     // rounds of 32 keys: this work-group's share of them, its wavefronts in turn
     const int rounds = (S.count + 31) / 32;
@@ -156,7 +132,7 @@ __global__ __launch_bounds__(WTHR, (dec_waves<T, D>())) void window_step_kernel(
     if (AHEAD && r0 + wave < r1) {
         load_k(32 * (r0 + wave));
 #pragma unroll
-        for (int i = 0; i < (AHEAD ? VBX : 0); ++i) load_v(32 * (r0 + wave), i, vr[AHEAD ? i : 0]);
+        for (int i = 0; i < (AHEAD ? VBX : 0); ++i) load_v(32 * (r0 + wave), i, &vr[AHEAD ? i : 0]);
     }
     for (int r = r0 + wave; r < r1; r += 4) {
         const int u0 = 32 * r;
@@ -165,11 +141,11 @@ __global__ __launch_bounds__(WTHR, (dec_waves<T, D>())) void window_step_kernel(
 #pragma unroll
             for (int s = 0; s < TL::KS; ++s) x = P::mma(kf[s], qf[s], x);
 #pragma unroll
-            for (int i = 0; i < VBX; ++i) store_v(i, vr[i]);
+            for (int i = 0; i < VBX; ++i) store_v(i, &vr[i]);
             if (r + 4 < r1) {
                 load_k(u0 + 128);
 #pragma unroll
-                for (int i = 0; i < VBX; ++i) load_v(u0 + 128, i, vr[i]);
+                for (int i = 0; i < VBX; ++i) load_v(u0 + 128, i, &vr[i]);
             }
         } else {
             const T* kr = row_of(min(u0 + col, S.count - 1), kcb, knb);
@@ -177,26 +153,23 @@ __global__ __launch_bounds__(WTHR, (dec_waves<T, D>())) void window_step_kernel(
             for (int s = 0; s < TL::KS; ++s) x = P::mma(load_piece(kr, 2 * s + hh), load_piece(qrow, 2 * s + hh), x);
 #pragma unroll 2
             for (int i = 0; i < VBX; ++i) {
-                u32x4 y[4];
-                load_v(u0, i, y);
-                store_v(i, y);
+                u32x4 y;
+                load_v(u0, i, &y);
+                store_v(i, &y);
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (CAP) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = tanhf(x[i] * ci);
-        }
+        own_fence();
+        if (CAP) tanh_scores<T>(x, ci);
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = u0 + 8 * (i / 4) + 4 * hh + i % 4 < S.count ? x[i] : -INFINITY;
             top = fmaxf(top, x[i]);
         }
-        top = fmaxf(top, other_half(top)) * c;
-        if (__any(top > m + LOWER + 8.f)) {
-            const float to = fmaxf(m, top - LOWER), f = exp2f(m - to);
+        top = halves_max(top) * c;
+        const bool over = top > m + LOWER + 8.f;
+        if (__any(over)) {
+            const float to = over ? top - LOWER : m, f = exp2f(m - to);
             m = to;
             l *= f;
 #pragma unroll
@@ -212,13 +185,12 @@ __global__ __launch_bounds__(WTHR, (dec_waves<T, D>())) void window_step_kernel(
         for (int s = 0; s < TL::US; ++s) {
             const u32x4 pf = P::pack(p + s * P::E);
 #pragma unroll
-            for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(TL::comps_piece(mine, db, 0, s, lane), pf, o[db]);
+            for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(TL::comps_piece(mine, cplace, db, s), pf, o[db]);
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        own_fence();
     }
     // the four wavefronts' softmaxes become one: a common reference, then the sums one after the other
-    l += other_half(l);
+    l = halves_sum(l);
     if (hh == 0) { s_m[wave][col] = m; s_l[wave][col] = l; }
     __syncthreads();                                          // (and LDS changes its use)
     float M = s_m[0][col];

@@ -34,7 +34,7 @@ def call(fn, ptrs=None, ws=1 << 40, capacity=64, **kw):
     (dict(n=1 << 25), focus.FOCUS_EUNSUPPORTED), (dict(Hq=512, Hkv=2), focus.FOCUS_EUNSUPPORTED), (dict(B=40000), focus.FOCUS_EUNSUPPORTED),
     (dict(scale=-1.0), focus.FOCUS_EINVAL), (dict(softcap=float("nan")), focus.FOCUS_EINVAL), (dict(span_max=257), focus.FOCUS_EINVAL),
     (dict(span_max=-1), focus.FOCUS_EINVAL), (dict(q_strides=(16384, 4096, 65)), focus.FOCUS_EINVAL),
-    (dict(kv_strides=(-8, 4096, 64)), focus.FOCUS_EINVAL)])
+    (dict(kv_strides=(-8, 4096, 64)), focus.FOCUS_EINVAL), (dict(o_strides=(64, 64, 1 << 24)), focus.FOCUS_EUNSUPPORTED)])
 def test_params_refused(fn, kw, want):
     st, msg = call(fn, **kw)
     assert st == want, msg
