@@ -326,30 +326,41 @@ __device__ inline void store_row(T* row, const f32x16* acc, float f, int lane)
 }
 
 // The keys that rows first .. last can see, in blocks of 32 and tiles of U blocks: the sinks' blocks, then those from the first key of the
-// window on.  (The last tile of the sinks may have fewer blocks, so that none is walked for nothing.)
+// window on.  (A single block of sinks has a tile to itself, more of them whole tiles; the blocks behind the last sink are window like any.)
 struct Walk {
     int first, last, sink_blocks, sink_tiles, base, blocks, tiles;
-    int lone_tile;              // the last tile of the sinks if it has one block where others have two: no step between its first and its last
     int open0;                  // keys from here to the first row hide nothing
     __device__ Walk(const WindowArgs& A, const Sequence& sq, int first_, int last_, int U)
     {
         first = first_;
         last = last_;
         sink_blocks = (min(A.sinks, last + 1) + 31) / 32;
+        if (sink_blocks > 1) sink_blocks = (sink_blocks + U - 1) / U * U;
         sink_tiles = (sink_blocks + U - 1) / U;
         base = max(32 * sink_blocks, max(0, first - A.window + 1) & ~31);
         const int near = max(0, last / 32 - base / 32 + 1);
         blocks = sink_blocks + near;
         tiles = sink_tiles + (near + U - 1) / U;
-        lone_tile = U == 2 && sink_blocks % 2 != 0 ? sink_tiles - 1 : -1;
         open0 = last - A.window + 1;
     }
+    __device__ int key_at(int t, int R) const { return t < sink_tiles ? t * R : base + (t - sink_tiles) * R; }
     // may a pair of the rows and keys key0 .. key0 + R - 1 be hidden?
     __device__ bool edge(int key0, int R, const WindowArgs& A) const
     {
         return key0 + R - 1 > first || (key0 < open0 && key0 + R - 1 >= A.sinks);
     }
 };
+// A block of a walk: tile and place in it
+struct At {
+    int t, u;
+};
+template <int U>
+__device__ inline At after(At a, const Walk& W)
+{
+    if (U == 1) return At{a.t + 1, 0};
+    const bool end = a.u == U - 1 || (a.t == 0 && W.sink_blocks == 1);
+    return At{end ? a.t + 1 : a.t, end ? 0 : a.u + 1};
+}
 
 // tanh of 16 scores times f: its series to z^9 while all are below 0.3 in magnitude (the next term is 1.6e-8 there, half a step of fp32
 // relative to z: six operations in place of an exponential and a reciprocal), else from exp(-2 |z|); fp32 takes the library's there.

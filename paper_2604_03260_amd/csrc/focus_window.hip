@@ -34,7 +34,10 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
                                                                              T* __restrict__ out, float* __restrict__ lse)
 {
     constexpr int R = key_tile<T, D>(), U = R / 32;           // keys and steps of a tile
-    constexpr int VLAG = U == 2 ? 1 : 2;                      // tiles that V is fetched behind K
+    // Operands of the products are read a step ahead where the registers hold them.  K is fetched KFETCH tiles ahead of the softmax, V VFETCH
+    constexpr bool AHEAD = D * (int)sizeof(T) <= 256;
+    static_assert(AHEAD || U == 1, "without operands ahead a tile is one block");
+    constexpr int KFETCH = AHEAD && U == 1 ? 3 : 2, VFETCH = AHEAD ? 1 : 0;
     typedef Tile<T, D, R> TL;
     typedef Piece<T> P;
     __shared__ __attribute__((aligned(256))) char s_k[2][TL::BYTES], s_v[2][TL::BYTES];
@@ -70,7 +73,7 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
     const float ci = CAP ? A.scale / A.softcap : 0.f;
 
     const Walk W(A, sq, tile0, min((four * 4 + 3) / G * 32 + 32, sq.len) - 1, U);
-    auto key_at = [&](int t) WINDOW_INLINE { return t < W.sink_tiles ? t * R : W.base + (t - W.sink_tiles) * R; };
+    auto key_at = [&](int t) WINDOW_INLINE { return W.key_at(t, R); };
     const int pitch = (int)(A.ks[2] * (long long)sizeof(T));
     Dma<T, D, R, 4> dma;
     dma.init(wave, lane, pitch);
@@ -79,12 +82,7 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
         const int key = key_at(min(t, W.tiles - 1));
         dma.load(base + (long long)key * A.ks[2], pitch, sq.len - key, bufs + (t & 1) * TL::BYTES, wave, lane);
     };
-    // in the last step of tile t: the next K and V on their way
-    auto turn = [&](int t) WINDOW_INLINE {
-        fetch(kb, s_k[0], t + 2);
-        fetch(vb, s_v[0], t + 2 - VLAG);
-    };
-    // V of tile t has landed and is about to be met
+    // V of tile t has landed and is about to be read
     auto check = [&](int t) WINDOW_INLINE {
         if (threadIdx.x < 2) s_bad[(t + 1) & 3][threadIdx.x] = 0u;
         if (t >= 0 && W.edge(key_at(t), R, A)) {
@@ -93,18 +91,22 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
         }
     };
     if (threadIdx.x < 8) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
-    for (int i = threadIdx.x; i < TL::BYTES / 16; i += WTHR) *(u32x4*)(s_v[1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};   // (met by weights of zero before it is filled)
     fetch(kb, s_k[0], 0);
     fetch(kb, s_k[0], 1);
-    if constexpr (U == 2) fetch(vb, s_v[0], 0);
+    if constexpr (AHEAD) fetch(vb, s_v[0], 0);
+    else
+        for (int i = threadIdx.x; i < TL::BYTES / 16; i += WTHR) *(u32x4*)(s_v[1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};   // (met by weights of zero)
     dma_wait();
     __syncthreads();
 
     const int rplace = TL::rows_place(lane), cplace = TL::comps_place(lane);
     f32x16 x = 0.f;                                           // scores of the step's block, then of the next one
     u32x4 pf[TL::US];                                         // probabilities of the block before
+    u32x4 ka[AHEAD ? TL::KS : 1], va[AHEAD ? TL::US * TL::DB : 1];
 #pragma unroll
     for (int s = 0; s < TL::US; ++s) pf[s] = 0u;
+#pragma unroll
+    for (int s = 0; s < (AHEAD ? TL::US * TL::DB : 1); ++s) va[s] = 0u;
     // hides what a row does not see, once the scores are there (blocks from key open0 to open1 hide nothing)
     const int open0 = row0 + 32 - A.window, open1 = row0 - 31;
     auto finish = [&](int key0) WINDOW_INLINE {
@@ -122,19 +124,10 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
         const unsigned marks = s_bad[t & 3][u];
         if (marks != 0u && spoiled_by<true>(marks, row, key + 32 * u, hh, A.window, A.sinks)) l = __builtin_nanf("");
     };
-    int tv = 1, uv = 0;                                       // tile and place of the block before (at first: the zeros)
-    // softmax of the scores x beside the next block's scores (K at kbuf) and the last block's values (V at vbuf).  The operands' reads first,
-    // then the softmax, then the products: the reads pass under the softmax, the products of one wavefront of a SIMD under the softmax
-    // of the other
+    // softmax of the scores x, then the next block's scores and the last block's values.  With operands ahead, those of the next step are read
+    // between the products, each into the registers that a product has just read: knext, vnext say where.  Else they are read where they are needed.
     auto products = [&](const char* kbuf, const char* vbuf) WINDOW_INLINE {
         const int rp = opaque(rplace), cp = opaque(cplace);
-        u32x4 va[TL::US * TL::DB], ka[TL::KS];
-#pragma unroll
-        for (int s = 0; s < TL::US; ++s)
-#pragma unroll
-            for (int db = 0; db < TL::DB; ++db) va[s * TL::DB + db] = TL::comps_piece(vbuf, cp, db, s);
-#pragma unroll
-        for (int s = 0; s < TL::KS; ++s) ka[s] = TL::rows_piece(kbuf, rp, s);
         __builtin_amdgcn_sched_barrier(0);
         float top = x[0];
 #pragma unroll
@@ -157,13 +150,39 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
             asm volatile("" : "+v"(pn[s]));                   // (found here, not behind the products)
         }
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int s = 0; s < TL::US; ++s)
-#pragma unroll
-            for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(va[s * TL::DB + db], pf[s], o[db]);
         x = 0.f;
+        if constexpr (AHEAD) {
 #pragma unroll
-        for (int s = 0; s < TL::KS; ++s) x = P::mma(ka[s], qf[s], x);
+            for (int s = 0; s < TL::KS; ++s) {
+                x = P::mma(ka[s], qf[s], x);
+                ka[s] = TL::rows_piece(kbuf, rp, s);
+            }
+#pragma unroll
+            for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+                for (int db = 0; db < TL::DB; ++db) {
+                    o[db] = P::mma(va[s * TL::DB + db], pf[s], o[db]);
+                    va[s * TL::DB + db] = TL::comps_piece(vbuf, cp, db, s);
+                }
+            constexpr int READS = sizeof(T) == 4 ? 4 : 2;
+#pragma unroll
+            for (int j = 0; j < TL::KS; ++j) {
+                __builtin_amdgcn_sched_group_barrier(0x008, sizeof(T) == 4 ? 4 : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < TL::US * TL::DB; ++j) {
+                __builtin_amdgcn_sched_group_barrier(0x008, sizeof(T) == 4 ? 4 : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < TL::KS; ++s) x = P::mma(TL::rows_piece(kbuf, rp, s), qf[s], x);
+#pragma unroll
+            for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+                for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(TL::comps_piece(vbuf, cp, db, s), pf[s], o[db]);
+        }
 #pragma unroll
         for (int s = 0; s < TL::US; ++s) pf[s] = pn[s];
         __builtin_amdgcn_sched_barrier(0);
@@ -172,41 +191,49 @@ __global__ __launch_bounds__(WTHR, (fwd_waves<T, D>())) void window_fwd_kernel(W
             for (int j = 0; j < TL::DB; ++j) o[j] *= f;
         }
     };
+    At before = {AHEAD ? 0 : 1, 0}, here = {0, 0}, next = after<U>(here, W);
+    auto kat = [&](At a) WINDOW_INLINE { return s_k[0] + (a.t & 1) * TL::BYTES + TL::BLOCK * a.u; };
+    auto vat = [&](At a) WINDOW_INLINE { return s_v[0] + (a.t & 1) * TL::BYTES + TL::BLOCK * a.u; };
 #pragma unroll
     for (int s = 0; s < TL::KS; ++s) x = P::mma(TL::rows_piece(s_k[0], rplace, s), qf[s], x);
     finish(key_at(0));
-    int t = 0, u = 0;
+    if constexpr (AHEAD) {
+#pragma unroll
+        for (int s = 0; s < TL::KS; ++s) ka[s] = TL::rows_piece(kat(next), rplace, s);
+        if constexpr (U == 1) {
+            __syncthreads();                                  // (K of tile 2 goes where that of tile 0 was)
+            fetch(kb, s_k[0], 2);
+        }
+    }
 #pragma unroll 1
     for (int i = 0; i < W.blocks; ++i) {
-        const bool lone = t == W.lone_tile, end = u == U - 1 || lone;
-        if (end) {
+        if (here.u == 0) {                                    // the first step of a tile
             dma_wait();
             __syncthreads();
-            check(U == 2 ? t : t - 1);
-            if (!lone) turn(t);
+            check(AHEAD ? here.t : here.t - 1);
+            fetch(kb, s_k[0], here.t + KFETCH);
+            fetch(vb, s_v[0], here.t + VFETCH);
         }
-        const int tk = end ? t + 1 : t, uk = end ? 0 : u + 1;           // (behind the last block: whatever is there, not used)
-        products(s_k[0] + (tk & 1) * TL::BYTES + TL::BLOCK * uk, s_v[0] + (tv & 1) * TL::BYTES + TL::BLOCK * uv);
-        finish(key_at(tk) + 32 * uk);
-        if (i > 0) look(tv, uv);
-        if (lone) {                                           // (this step has read the buffer that the next V goes to)
-            __syncthreads();
-            turn(t);
-        }
-        tv = t;
-        uv = u;
-        t = tk;
-        u = uk;
+        const At third = after<U>(next, W);
+        if constexpr (AHEAD) products(kat(third), vat(here));
+        else products(kat(next), vat(before));
+        finish(key_at(next.t) + 32 * next.u);
+        if (i > 0) look(before.t, before.u);
+        before = here;
+        here = next;
+        next = third;
     }
     dma_wait();                                               // (nothing may land in LDS after the work-group's end)
-    __syncthreads();
-    check(tv);
+    if constexpr (!AHEAD) {
+        __syncthreads();
+        check(before.t);
+    }
     if (row0 >= sq.len) return;
 #pragma unroll
     for (int s = 0; s < TL::US; ++s)
 #pragma unroll
-        for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(TL::comps_piece(s_v[0] + (tv & 1) * TL::BYTES + TL::BLOCK * uv, cplace, db, s), pf[s], o[db]);
-    look(tv, uv);
+        for (int db = 0; db < TL::DB; ++db) o[db] = P::mma(AHEAD ? va[AHEAD ? s * TL::DB + db : 0] : TL::comps_piece(vat(before), cplace, db, s), pf[s], o[db]);
+    look(before.t, before.u);
     l = halves_sum(l);
     T* orow = real ? out + (long long)sq.tb * A.os[0] + (long long)h * A.os[1] + (long long)(sq.first + row) * A.os[2] : nullptr;
     store_row<T, D>(orow, o, 1.f / l, lane);
