@@ -281,23 +281,25 @@ __global__ __launch_bounds__(RTHR) void rope_kernel(RopeArgs A)
     }
 }
 
-// dw[i] = sum of the partial sums of q's (blockIdx.y 0) or k's slots, in 64 bits and in one order: 16 components per work-group,
-// 16 lanes for each.
-__global__ __launch_bounds__(RTHR) void rope_dw_kernel(const float* __restrict__ partial, int qslots, int kslots, int d,
-                                                       float* __restrict__ dwq, float* __restrict__ dwk)
+// dw[i] = sum of the partial sums of q's (blockIdx.y 0) or k's slots, in 64 bits and in one order: 16 components per work-group, 64 shares of
+// the slots for each.
+constexpr int DW_THR = 1024;
+__global__ __launch_bounds__(DW_THR) void rope_dw_kernel(const float* __restrict__ partial, int qslots, int kslots, int d,
+                                                        float* __restrict__ dwq, float* __restrict__ dwk)
 {
-    __shared__ double s[16][17];
-    const int i = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
+    __shared__ double s[64][16];
+    const int c = threadIdx.x % 16, i = blockIdx.x * 16 + c, part = threadIdx.x / 16;
     const int first = blockIdx.y ? qslots : 0, count = blockIdx.y ? kslots : qslots;
     double sum = 0.0;
-    for (int j = part; j < count; j += 16) sum += (double)partial[(size_t)(first + j) * d + i];
-    s[part][threadIdx.x % 16] = sum;
+#pragma unroll 8
+    for (int j = part; j < count; j += 64) sum += (double)partial[(size_t)(first + j) * d + i];
+    s[part][c] = sum;
     __syncthreads();
-    if (part == 0) {
-        double total = 0.0;
-        for (int j = 0; j < 16; ++j) total += s[j][threadIdx.x];
-        (blockIdx.y ? dwk : dwq)[i] = (float)total;
+    for (int half = 32; half > 0; half /= 2) {
+        if (part < half) s[part][c] += s[part + half][c];
+        __syncthreads();
     }
+    if (part == 0) (blockIdx.y ? dwk : dwq)[i] = (float)s[0][c];
 }
 
 template <int OP, typename T, int LAY>
@@ -342,7 +344,7 @@ int heads_per_chunk(const RopeArgs& A)
 static int bwd_blocks(const RopeArgs& A, int chunks)
 {
     const long long tpb = RTHR / lanes_per_row(A.d), blocks = ((long long)A.B * A.n + tpb - 1) / tpb;
-    return (int)std::max(1ll, std::min(blocks, (long long)std::max(1, 2048 / chunks)));
+    return (int)std::max(1ll, std::min(blocks, (long long)std::max(1, 1024 / chunks)));
 }
 
 size_t rope_bwd_workspace(const RopeArgs& A0)
@@ -362,7 +364,7 @@ hipError_t launch_rope(const RopeArgs& A0, int op, hipStream_t st)
         const int bx = bwd_blocks(A, chunks);
         hipError_t e = launch_type<2>(A, dim3(bx, chunks), st);
         if (e != hipSuccess) return e;
-        rope_dw_kernel<<<dim3(A.d / 16, A.Hkv > 0 ? 2 : 1), RTHR, 0, st>>>(A.partial, qchunks * bx, (chunks - qchunks) * bx, A.d,
+        rope_dw_kernel<<<dim3(A.d / 16, A.Hkv > 0 ? 2 : 1), DW_THR, 0, st>>>(A.partial, qchunks * bx, (chunks - qchunks) * bx, A.d,
                                                                           A.q.dw, A.k.dw);
         return hipGetLastError();
     }

@@ -216,7 +216,7 @@ template <typename T, int D, int R>
 __device__ inline void scrub(char* tile, unsigned* bad)
 {
     typedef Tile<T, D, R> TL;
-    for (int id = threadIdx.x; id < TL::BYTES / 16; id += WTHR) {
+    for (int id = threadIdx.x; id < TL::BYTES / 16; id += blockDim.x) {
         u32x4 v = *(const u32x4*)(tile + 16 * id);
         bool found = false;
 #pragma unroll

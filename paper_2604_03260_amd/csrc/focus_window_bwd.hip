@@ -20,10 +20,9 @@ using namespace window;
 
 namespace {
 
-// Keys of a dq tile: 32, so that two work-groups share a compute unit's LDS.  Rows of a dkv tile: its operands leave room for one wavefront per
-// SIMD only, and one work-group may have all of LDS.
+// Keys of a dq tile: 32, so that two work-groups share a compute unit's LDS.  Rows of a dkv tile: what eight wavefronts fill evenly.
 constexpr int DQ_TILE = 32;
-template <typename T, int D> constexpr int dkv_tile() { return sizeof(T) == 4 || D > 128 ? 32 : 64; }
+template <typename T, int D> constexpr int dkv_tile() { return D * (int)sizeof(T) > 512 || (sizeof(T) == 4 && (D == 64 || D == 128)) ? 32 : 64; }
 template <typename T, int D> constexpr int dq_waves() { return D * (int)sizeof(T) > 256 ? 1 : 2; }
 
 constexpr int KEYS = 128;                   // keys of a dkv work-group
@@ -256,64 +255,69 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
     store_row<T, D>(real ? dq + qoff : nullptr, acc, A.scale + spoiled, lane);
 }
 
-// P and dS of a lane's 16 pairs from its scores (tanh of them with a softcap) and dP, packed as operands.  ls, dl: the log-sum-exps (log2 units)
-// and deltas of the 16 rows, in LDS.  A pair that is hidden has a score of -inf (softcap: -1e30) and dP = 0.
+// P of a lane's 16 pairs from its scores (tanh of them with a softcap), or dS from these and dP (grad), packed as operands.  ls, dl: the
+// log-sum-exps (log2 units) and deltas of the 16 rows, in LDS.  A pair that is hidden has a score of -inf (softcap: -1e30) and dP = 0.
 template <typename T, bool CAP>
-__device__ inline void probabilities(const f32x16& x, const f32x16& dp, float c, const float* ls, const float* dl, int hh, u32x4* pf, u32x4* df)
+__device__ inline void probabilities(const f32x16& x, const f32x16& dp, float c, const float* ls, const float* dl, int hh, bool grad, u32x4* out)
 {
     typedef Piece<T> P;
     constexpr int US = 16 / P::E;
+    float p[16];
 #pragma unroll
-    for (int s = 0; s < US; ++s) {
-        float p[8], ds[8];
+    for (int m = 0; m < 4; ++m) {
+        const float4 l4 = *(const float4*)(ls + 8 * m + 4 * hh);
+        const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
-        for (int m = 0; m < P::E / 4; ++m) {
-            const int at = 8 * (s * P::E / 4 + m) + 4 * hh;
-            const float4 l4 = *(const float4*)(ls + at), d4 = *(const float4*)(dl + at);
-            const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+        for (int j = 0; j < 4; ++j) p[4 * m + j] = __builtin_amdgcn_exp2f(fmaf(x[4 * m + j], c, -lv[j]));
+    }
+    if (grad) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const float4 d4 = *(const float4*)(dl + 8 * m + 4 * hh);
+            const float dv[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int i = s * P::E + 4 * m + j;
-                const float e = __builtin_amdgcn_exp2f(fmaf(x[i], c, -lv[j]));
-                p[4 * m + j] = e;
-                ds[4 * m + j] = e * (dp[i] - dv[j]);
-                if (CAP) ds[4 * m + j] = x[i] > -2.f ? ds[4 * m + j] * (1.f - x[i] * x[i]) : 0.f;
+                const int i = 4 * m + j;
+                p[i] *= dp[i] - dv[j];
+                if (CAP) p[i] = x[i] > -2.f ? p[i] * (1.f - x[i] * x[i]) : 0.f;
             }
         }
-        pf[s] = P::pack(p);
-        df[s] = P::pack(ds);
     }
+#pragma unroll
+    for (int s = 0; s < US; ++s) out[s] = P::pack(p + s * P::E);
 }
 
 // The rows from a key tile's own to the end of its window, of every query head; to dk and dv, or, where far rows follow, in 32 bits to `part`.
-// Step i: S and dP of block i + 1, P and dS of block i, dV += dout^T P and dK += Q^T dS of block i - 1 (rows in two buffers, as in the
-// forward kernel: by rows ahead, by components behind).
+// Two wavefronts fit a SIMD if the sums of one are those of dK or of dV (dkv_split; not at 64 components of 16 bits): eight wavefronts, two for
+// each 32 keys.  Both find the scores (ten products of a block in place of eight), but with one that held all sums, every wait, barrier and
+// vector instruction was in the way of the products (16384 tokens of 32/8 heads of 128, window 1024: 1214 us, split 995; at 64 components,
+// 8 x 4096 tokens of 12 heads, window 256: 165 us with both, split 277).
+template <typename T, int D> constexpr bool dkv_split() { return D * (int)sizeof(T) > 128; }
+template <typename T, int D> constexpr int dkv_threads() { return dkv_split<T, D>() ? 512 : 256; }
 template <typename T, int D, bool CAP>
-__global__ __launch_bounds__(WTHR, (D * (int)sizeof(T) <= 128 ? 2 : 1)) void window_dkv_kernel(WindowArgs A, FarPlan F, int tiles, const T* __restrict__ q, const T* __restrict__ k,
-                                                           const T* __restrict__ v, const float* __restrict__ lse,
-                                                           const T* __restrict__ dout, const float* __restrict__ delta,
-                                                           float* __restrict__ part, T* __restrict__ dk, T* __restrict__ dv)
+__global__ __launch_bounds__((dkv_threads<T, D>()), 2) void window_dkv_kernel(WindowArgs A, FarPlan F, int tiles, const T* __restrict__ q, const T* __restrict__ k,
+                                                              const T* __restrict__ v, const float* __restrict__ lse,
+                                                              const T* __restrict__ dout, const float* __restrict__ delta,
+                                                              float* __restrict__ part, T* __restrict__ dk, T* __restrict__ dv)
 {
     constexpr int R = dkv_tile<T, D>(), U = R / 32;
     typedef Tile<T, D, R> TL;
     typedef Piece<T> P;
-    // the keys' and values' operands stay in registers where they fit; above 256 bytes a row they are read again from L1 for every block.
-    // Rows of 1024 bytes do not fit LDS often enough: by rows they are read from L1 too
-    constexpr bool KEEP = D * (int)sizeof(T) <= 256, ROWS = D * (int)sizeof(T) <= 512;
-    // tiles from before their scores to behind their sums
-    constexpr int NB = !ROWS ? 2 : U == 2 ? 3 : 4;
-    __shared__ __attribute__((aligned(256))) char s_q[NB][TL::BYTES], s_g[NB][TL::BYTES];
-    __shared__ __attribute__((aligned(16))) float s_lse[4][R], s_del[4][R];
-    __shared__ unsigned s_bad[4][2], s_lost[4][2];
+    // the keys' and values' operands stay in registers where they fit; above 256 bytes a row they are read again from L1 for every block
+    constexpr bool KEEP = D * (int)sizeof(T) <= 256, SPLIT = dkv_split<T, D>();
+    __shared__ __attribute__((aligned(256))) char s_q[2][TL::BYTES], s_g[2][TL::BYTES];
+    __shared__ __attribute__((aligned(16))) float s_lse[2][R], s_del[2][R];
+    __shared__ unsigned s_bad[2][2], s_lost[2][2];
     const int lane = threadIdx.x & 63, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool sum_k = !SPLIT || wave >= 4, sum_v = !SPLIT || wave < 4;
     const int G = A.Hq / A.Hkv;
     const long long w = work_of((long long)A.B * A.Hkv * tiles);
     if (w < 0) return;
     const int tile = (int)(w % tiles), hk = (int)(w / tiles % A.Hkv), b = (int)(w / tiles / A.Hkv);
     const Sequence sq = sequence_of(A, b);
     if (tile * KEYS >= sq.len) return;
-    const int tkey = tile * KEYS, key0 = tkey + 32 * wave;    // keys of the work-group, of the wavefront
+    const int tkey = tile * KEYS, key0 = tkey + 32 * (wave & 3);        // keys of the work-group, of the wavefront
     const int from = tkey, to = min(far_start(tile, A.window), sq.len);
     const int key = key0 + (lane & 31);
     const bool real = key < sq.len;
@@ -328,29 +332,30 @@ __global__ __launch_bounds__(WTHR, (D * (int)sizeof(T) <= 128 ? 2 : 1)) void win
         }
     }
     float spoiled = 0.f;                                      // or NaN
-    f32x16 ak[TL::DB], av[TL::DB];
+    f32x16 acc[TL::DB], both[SPLIT ? 1 : TL::DB];             // dK or dV; dV beside dK
 #pragma unroll
-    for (int i = 0; i < TL::DB; ++i) ak[i] = av[i] = 0.f;
+    for (int i = 0; i < TL::DB; ++i) acc[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < (SPLIT ? 1 : TL::DB); ++i) both[i] = 0.f;
     const float c = CAP ? A.softcap * LOG2E : A.scale * LOG2E;
     const float ci = CAP ? A.scale / A.softcap : 0.f;
 
     // the walk: tiles of R rows, head after head, th of each head (rows behind `to` in the last one are hidden)
     const int th = (to - from + R - 1) / R, ntiles = th * G;
-    // a tile of the walk: head, first row (from + j R), and where its rows and sums lie
+    // a tile of the walk: first row (from + j R), and where its rows and sums lie
     struct Cursor {
         int t, j, row;
         const T *q, *g;
         long long sums;
     };
     const long long qhead = A.qs[1], ghead = A.os[1], qstep = (long long)R * A.qs[2], gstep = (long long)R * A.os[2];
-    Cursor start;
-    start.t = start.j = 0;
-    start.row = from;
-    start.q = q + (long long)sq.tb * A.qs[0] + (long long)hk * G * qhead + (long long)(sq.first + from) * A.qs[2];
-    start.g = dout + (long long)sq.tb * A.os[0] + (long long)hk * G * ghead + (long long)(sq.first + from) * A.os[2];
-    start.sums = ((long long)sq.tb * A.Hq + hk * G) * A.n + sq.first + from;
-    auto advance = [&](Cursor& c) WINDOW_INLINE {              // (behind the last tile it stays there)
-        if (c.t + 1 >= ntiles) return;
+    Cursor next;                                              // the next tile to be fetched
+    next.t = next.j = 0;
+    next.row = from;
+    next.q = q + (long long)sq.tb * A.qs[0] + (long long)hk * G * qhead + (long long)(sq.first + from) * A.qs[2];
+    next.g = dout + (long long)sq.tb * A.os[0] + (long long)hk * G * ghead + (long long)(sq.first + from) * A.os[2];
+    next.sums = ((long long)sq.tb * A.Hq + hk * G) * A.n + sq.first + from;
+    auto advance = [&](Cursor& c) WINDOW_INLINE {
         ++c.t;
         if (++c.j < th) {
             c.row += R;
@@ -367,218 +372,118 @@ __global__ __launch_bounds__(WTHR, (D * (int)sizeof(T) <= 128 ? 2 : 1)) void win
         }
     };
     const int qpitch = (int)(A.qs[2] * (long long)sizeof(T)), gpitch = (int)(A.os[2] * (long long)sizeof(T));
-    Dma<T, D, R, 4> qdma, gdma;
+    Dma<T, D, R, SPLIT ? 8 : 4> qdma, gdma;
     qdma.init(wave, lane, qpitch);
     gdma.init(wave, lane, gpitch);
-    float nlse = 0.f, ndel = 0.f;
-    Cursor crows = start, csums = start;                      // the next tiles to be fetched
-    int tsums = 0;                                            // and to be put (running on behind the last one)
-    int brows = 0;                                            // buffer of the next rows
     auto edge_row = [&](int row) WINDOW_INLINE { return row < tkey + KEYS || row + R - 1 - tkey >= A.window; };
-    auto next_buffer = [&](int b) WINDOW_INLINE { return b + 1 == NB ? 0 : b + 1; };
-    auto fetch_rows = [&]() WINDOW_INLINE {
-        qdma.load(crows.q, qpitch, to - crows.row, s_q[0] + brows * TL::BYTES, wave, lane);
-        gdma.load(crows.g, gpitch, to - crows.row, s_g[0] + brows * TL::BYTES, wave, lane);
-        brows = next_buffer(brows);
-        advance(crows);
-    };
-    // the rows of tile t (first row `row`, in buffer b) have landed and are about to be met
-    auto check = [&](int t, int row, int b) WINDOW_INLINE {
-        if (threadIdx.x < 2) s_bad[(t + 1) & 3][threadIdx.x] = 0u;
-        if (t >= 0 && t < ntiles && edge_row(row)) {
-            scrub<T, D, R>(s_q[0] + b * TL::BYTES, s_bad[t & 3]);
-            scrub<T, D, R>(s_g[0] + b * TL::BYTES, s_bad[t & 3]);
-            __syncthreads();
-        }
-    };
-    bool sums_edge = false;
-    int sums_row = 0;
-    auto fetch_sums = [&]() WINDOW_INLINE {
-        sums_edge = edge_row(csums.row);
-        sums_row = csums.row;
+    float nlse = 0.f, ndel = 0.f;
+    auto fetch = [&]() WINDOW_INLINE {                         // rows, log-sum-exps and deltas of a tile
+        const int buf = next.t & 1;
+        qdma.load(next.q, qpitch, to - next.row, s_q[buf], wave, lane);
+        gdma.load(next.g, gpitch, to - next.row, s_g[buf], wave, lane);
         if (wave == 0 && lane < R) {
-            const bool there = csums.row + lane < to;
-            nlse = there ? lse[csums.sums + lane] * LOG2E : INFINITY;   // a row that is not there has probabilities of zero
-            ndel = there ? delta[csums.sums + lane] : 0.f;
+            const bool there = next.row + lane < to;
+            nlse = there ? lse[next.sums + lane] * LOG2E : INFINITY;    // a row that is not there has probabilities of zero
+            ndel = there ? delta[next.sums + lane] : 0.f;
         }
-        advance(csums);
     };
     // (a row whose sums are not finite would spoil keys that do not see it: in a tile with hidden pairs it is taken out and marked)
-    auto put_sums = [&]() WINDOW_INLINE {
-        if (wave == 0) {
-            bool lost = false;
-            if (sums_edge) {
-                lost = lane < R && sums_row + lane < to && !(fabsf(nlse) < INFINITY && fabsf(ndel) < INFINITY);
-                nlse = lost ? INFINITY : nlse;
-                ndel = lost ? 0.f : ndel;
-            }
-            const unsigned long long all = __ballot(lost);
-            if (lane == 0) { s_lost[tsums & 3][0] = (unsigned)all; s_lost[tsums & 3][1] = (unsigned)(all >> 32); }
-            if (lane < R) { s_lse[tsums & 3][lane] = nlse; s_del[tsums & 3][lane] = ndel; }
+    auto put_sums = [&](int t, int row) WINDOW_INLINE {
+        if (wave != 0) return;
+        bool lost = false;
+        if (edge_row(row)) {
+            lost = lane < R && row + lane < to && !(fabsf(nlse) < INFINITY && fabsf(ndel) < INFINITY);
+            nlse = lost ? INFINITY : nlse;
+            ndel = lost ? 0.f : ndel;
         }
-        ++tsums;
+        const unsigned long long all = __ballot(lost);
+        if (lane == 0) { s_lost[t & 1][0] = (unsigned)all; s_lost[t & 1][1] = (unsigned)(all >> 32); }
+        if (lane < R) { s_lse[t & 1][lane] = nlse; s_del[t & 1][lane] = ndel; }
     };
-    if (threadIdx.x < 8) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
-    for (int i = threadIdx.x; i < TL::BYTES / 16; i += WTHR) {          // (met by weights of zero before they are filled)
-        *(u32x4*)(s_q[NB - 1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};
-        *(u32x4*)(s_g[NB - 1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};
-    }
-    if constexpr (ROWS) {
-        fetch_rows();
-        fetch_rows();
-    }
-    fetch_sums();
-    put_sums();
-    fetch_sums();
-    put_sums();
-    fetch_sums();
-    dma_wait();
-    __syncthreads();
-    if constexpr (ROWS) check(0, from, 0);
-
+    if (threadIdx.x < 4) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
+    fetch();
     const int rplace = TL::rows_place(lane), cplace = TL::comps_place(lane);
-    f32x16 x, dx;
-    u32x4 pf[TL::US], df[TL::US];
-#pragma unroll
-    for (int s = 0; s < TL::US; ++s) pf[s] = df[s] = 0u;
-    // operands of the scores' products from LDS, or from memory (rows row0 .. of the head at qr, gr)
-    auto row_piece = [&](const char* buf, const T* base, long long stride, int row0, int rp, int s) WINDOW_INLINE {
-        return ROWS ? TL::rows_piece(buf, rp, s) : load_piece(base + (long long)min(lane & 31, to - 1 - row0) * stride, 2 * s + hh);
-    };
-    auto key_piece = [&](const u32x4* kept, const T* base, int s) WINDOW_INLINE { return KEEP ? kept[KEEP ? s : 0] : load_piece(base + koff, 2 * s + hh); };
-    const int open0 = key0 + 31, open1 = key0 - 32 + A.window;           // blocks from row open0 to open1 hide nothing
-    auto finish = [&](int row0) WINDOW_INLINE {
-        if (CAP) tanh_scores<T>(x, ci);
-        if (row0 >= open0 && row0 <= open1 && row0 + 32 <= to) return;
-        const int row = opaque(row0 + 4 * hh);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = row + 8 * (i / 4) + i % 4;
-            const bool seen = (bool)((int)(r < to) & (int)visible(r, key, A.window, A.sinks));
-            x[i] = seen ? x[i] : CAP ? -1e30f : -INFINITY;
-            dx[i] = seen ? dx[i] : 0.f;
-        }
-    };
-    auto look = [&](int t, int u, int row0) WINDOW_INLINE {
-        if (!edge_row(row0 - 32 * u)) return;
-        const unsigned marks = s_bad[t & 3][u] | s_lost[t & 3][u];
-        if (marks != 0u && spoiled_by<false>(marks, key, row0, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
-    };
-    {
-        const int rp = opaque(rplace);
-        x = 0.f;
-        dx = 0.f;
-#pragma unroll
-        for (int s = 0; s < TL::KS; ++s) {
-            x = P::mma(row_piece(s_q[0], start.q, A.qs[2], from, rp, s), key_piece(kf, k, s), x);
-            dx = P::mma(row_piece(s_g[0], start.g, A.os[2], from, rp, s), key_piece(vf, v, s), dx);
-        }
-    }
-    finish(from);
-    Cursor here = start;
-    int tv = 0, uv = 0, rowv = -1, bv = NB - 1, bh = 0, t = 0;           // the block before: tile, place, row, buffer (none yet: the zeros); this one's buffer
 #pragma unroll 1
-    for (; t < ntiles; ++t) {
-        Cursor ahead = here;
-        advance(ahead);
-#pragma unroll
+    for (int t = 0; t < ntiles; ++t) {
+        const int row_t = next.row, buf = t & 1;
+        put_sums(t, row_t);                                   // (read two tiles ago, before a barrier)
+        dma_wait();
+        __syncthreads();
+        const bool edge = edge_row(row_t);
+        if (edge) {
+            scrub<T, D, R>(s_q[buf], s_bad[buf]);
+            scrub<T, D, R>(s_g[buf], s_bad[buf]);
+            __syncthreads();
+        }
+        advance(next);
+        if (t + 1 < ntiles) fetch();
+#pragma unroll 1
         for (int u = 0; u < U; ++u) {
-            if (u == U - 1) {
-                // the last step of tile t: the next rows on their way
-                dma_wait();
-                __syncthreads();
-                if constexpr (ROWS) check(t + 1, ahead.row, next_buffer(bh));
-                else check(t - 1, rowv, bv);
-                put_sums();
-                fetch_rows();
-                fetch_sums();
-            }
-            const bool same = u + 1 < U;
-            const int rowk = same ? here.row + 32 * (u + 1) : ahead.row, bk = same ? bh : next_buffer(bh);
-            const char *qk = s_q[0] + bk * TL::BYTES + (same ? TL::BLOCK * (u + 1) : 0), *gk = s_g[0] + bk * TL::BYTES + (same ? TL::BLOCK * (u + 1) : 0);
-            const char *qv = s_q[0] + bv * TL::BYTES + TL::BLOCK * uv, *gv = s_g[0] + bv * TL::BYTES + TL::BLOCK * uv;
+            const int row0 = row_t + 32 * u;
+            const Block kind = row0 >= to ? HIDDEN : block_kind(row0, key0, A.window, A.sinks);
+            if (kind == HIDDEN) continue;
+            const char *qb = s_q[buf] + TL::BLOCK * u, *gb = s_g[buf] + TL::BLOCK * u;
             const int rp = opaque(rplace), cp = opaque(cplace);
-            // reads, then the vector work, then the products (KEEP: all operands wait in registers)
-            u32x4 ca[KEEP ? 2 * TL::US * TL::DB : 1], ra[KEEP ? 2 * TL::KS : 1];
-            if constexpr (KEEP) {
+            f32x16 x = 0.f, dx = 0.f;
+#pragma unroll
+            for (int s = 0; s < TL::KS; ++s) x = P::mma(TL::rows_piece(qb, rp, s), KEEP ? kf[KEEP ? s : 0] : load_piece(k + koff, 2 * s + hh), x);
+            if (sum_k) {
+#pragma unroll
+                for (int s = 0; s < TL::KS; ++s) dx = P::mma(TL::rows_piece(gb, rp, s), KEEP ? vf[KEEP ? s : 0] : load_piece(v + koff, 2 * s + hh), dx);
+            }
+            if (CAP) tanh_scores<T>(x, ci);
+            if (kind == EDGE || row0 + 32 > to) {
+                const int row = opaque(row0 + 4 * hh);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int r = row + 8 * (i / 4) + i % 4;
+                    const bool seen = (bool)((int)(r < to) & (int)visible(r, key, A.window, A.sinks));
+                    x[i] = seen ? x[i] : CAP ? -1e30f : -INFINITY;
+                    dx[i] = seen ? dx[i] : 0.f;
+                }
+            }
+            const float *ls = &s_lse[buf][32 * u], *dl = &s_del[buf][32 * u];
+            u32x4 w4[TL::US];
+            if constexpr (SPLIT) {
+                probabilities<T, CAP>(x, dx, c, ls, dl, hh, sum_k, w4);
+                const char* tb = sum_k ? qb : gb;
+#pragma unroll
+                for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+                    for (int db = 0; db < TL::DB; ++db) acc[db] = P::mma(TL::comps_piece(tb, cp, db, s), w4[s], acc[db]);
+            } else {
+                u32x4 p4[TL::US];
+                probabilities<T, CAP>(x, dx, c, ls, dl, hh, false, p4);
+                probabilities<T, CAP>(x, dx, c, ls, dl, hh, true, w4);
 #pragma unroll
                 for (int s = 0; s < TL::US; ++s)
 #pragma unroll
                     for (int db = 0; db < TL::DB; ++db) {
-                        ca[2 * (s * TL::DB + db)] = TL::comps_piece(gv, cp, db, s);
-                        ca[2 * (s * TL::DB + db) + 1] = TL::comps_piece(qv, cp, db, s);
+                        both[db] = P::mma(TL::comps_piece(gb, cp, db, s), p4[s], both[db]);
+                        acc[db] = P::mma(TL::comps_piece(qb, cp, db, s), w4[s], acc[db]);
                     }
-#pragma unroll
-                for (int s = 0; s < TL::KS; ++s) {
-                    ra[2 * s] = TL::rows_piece(qk, rp, s);
-                    ra[2 * s + 1] = TL::rows_piece(gk, rp, s);
-                }
             }
-            u32x4 pn[TL::US], dn[TL::US];
-            probabilities<T, CAP>(x, dx, c, &s_lse[t & 3][32 * u], &s_del[t & 3][32 * u], hh, pn, dn);
-#pragma unroll
-            for (int s = 0; s < TL::US; ++s)
-#pragma unroll
-                for (int db = 0; db < TL::DB; ++db) {
-                    const int at = KEEP ? 2 * (s * TL::DB + db) : 0;
-                    av[db] = P::mma(KEEP ? ca[at] : TL::comps_piece(gv, cp, db, s), pf[s], av[db]);
-                    ak[db] = P::mma(KEEP ? ca[KEEP ? at + 1 : 0] : TL::comps_piece(qv, cp, db, s), df[s], ak[db]);
-                }
-            x = 0.f;
-            dx = 0.f;
-#pragma unroll
-            for (int s = 0; s < TL::KS; ++s) {
-                const T *qr = (same ? here.q : ahead.q) + (same ? 32 * (u + 1) * A.qs[2] : 0), *gr = (same ? here.g : ahead.g) + (same ? 32 * (u + 1) * A.os[2] : 0);
-                x = P::mma(KEEP ? ra[KEEP ? 2 * s : 0] : row_piece(qk, qr, A.qs[2], rowk, rp, s), key_piece(kf, k, s), x);
-                dx = P::mma(KEEP ? ra[KEEP ? 2 * s + 1 : 0] : row_piece(gk, gr, A.os[2], rowk, rp, s), key_piece(vf, v, s), dx);
+            if (edge) {
+                const unsigned marks = s_bad[buf][u] | s_lost[buf][u];
+                if (marks != 0u && spoiled_by<false>(marks, key, row0, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
             }
-            if constexpr (KEEP) {
-#pragma unroll
-                for (int s = 0; s < TL::US; ++s) asm volatile("" : "+v"(pn[s]), "+v"(dn[s]));
-                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-                for (int j = 0; j < 2 * TL::KS + 2 * TL::US * TL::DB; ++j) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int s = 0; s < TL::US; ++s) { pf[s] = pn[s]; df[s] = dn[s]; }
-            finish(rowk);
-            if (rowv >= 0) look(tv, uv, rowv);
-            tv = t;
-            uv = u;
-            rowv = here.row + 32 * u;
-            bv = bh;
         }
-        here = ahead;
-        bh = next_buffer(bh);
+        if (edge) {                                           // (the marks have been seen by all before they go)
+            __syncthreads();
+            if (threadIdx.x < 2) s_bad[buf][threadIdx.x] = 0u;
+        }
     }
-    dma_wait();
-    __syncthreads();
-    if constexpr (!ROWS) check(tv, rowv, bv);
-    {
-        const int cp = opaque(cplace);
-        const char *qv = s_q[0] + bv * TL::BYTES + TL::BLOCK * uv, *gv = s_g[0] + bv * TL::BYTES + TL::BLOCK * uv;
-#pragma unroll
-        for (int s = 0; s < TL::US; ++s)
-#pragma unroll
-            for (int db = 0; db < TL::DB; ++db) {
-                av[db] = P::mma(TL::comps_piece(gv, cp, db, s), pf[s], av[db]);
-                ak[db] = P::mma(TL::comps_piece(qv, cp, db, s), df[s], ak[db]);
-            }
-    }
-    look(tv, uv, rowv);
     spoiled = halves_sum(spoiled);
-    if (F.any && tile < F.near_tiles) {
-        float* at = part + F.off_near / sizeof(float) + (((size_t)b * A.Hkv + hk) * F.near_tiles + tile) * 2 * KEYS * D + (size_t)(key - tkey) * D;
-        store_row<float, D>(real ? at : nullptr, ak, A.scale + spoiled, lane);
-        store_row<float, D>(real ? at + (size_t)KEYS * D : nullptr, av, 1.f + spoiled, lane);
-    } else {
-        store_row<T, D>(real ? dk + koff : nullptr, ak, A.scale + spoiled, lane);
-        store_row<T, D>(real ? dv + koff : nullptr, av, 1.f + spoiled, lane);
+    const bool sum_here = F.any && tile < F.near_tiles;
+    float* at = part + F.off_near / sizeof(float) + (((size_t)b * A.Hkv + hk) * F.near_tiles + tile) * 2 * KEYS * D + (size_t)(key - tkey) * D;
+    if (sum_k) {
+        if (sum_here) store_row<float, D>(real ? at : nullptr, acc, A.scale + spoiled, lane);
+        else store_row<T, D>(real ? dk + koff : nullptr, acc, A.scale + spoiled, lane);
+    }
+    if (sum_v) {
+        const f32x16* sums = SPLIT ? acc : both;
+        if (sum_here) store_row<float, D>(real ? at + (size_t)KEYS * D : nullptr, sums, 1.f + spoiled, lane);
+        else store_row<T, D>(real ? dv + koff : nullptr, sums, 1.f + spoiled, lane);
     }
 }
 
@@ -660,7 +565,8 @@ __global__ __launch_bounds__((64 * far_waves<T, D>()), 1) void window_far_kernel
             dx[i] = there ? dx[i] : 0.f;
         }
         u32x4 pf[TL::US], df[TL::US];
-        probabilities<T, CAP>(x, dx, c, ls, dl, hh, pf, df);
+        probabilities<T, CAP>(x, dx, c, ls, dl, hh, false, pf);
+        probabilities<T, CAP>(x, dx, c, ls, dl, hh, true, df);
 #pragma unroll
         for (int s = 0; s < TL::US; ++s)
 #pragma unroll
@@ -693,41 +599,51 @@ __global__ __launch_bounds__((64 * far_waves<T, D>()), 1) void window_far_kernel
     }
 }
 
-// dk and dv of the key tiles that hold sinks: the owner's sums, then the far chunks' head by head and chunk by chunk (in four shares, joined in
-// order).  One work-group per (b, KV head, key), 64 components of dk or dv at a time.
+// dk and dv of the key tiles that hold sinks: the owner's sums, then the far chunks' head by head and chunk by chunk.  A sink takes a work-group, its
+// far sums in 16 shares that are joined in order; the other keys of these tiles 16 to a work-group, rounded.
+constexpr int JOIN_THR = 1024;
 template <typename T>
-__global__ __launch_bounds__(WTHR) void window_join_kernel(WindowArgs A, FarPlan F, const float* __restrict__ part, T* __restrict__ dk,
-                                                          T* __restrict__ dv)
+__global__ __launch_bounds__(JOIN_THR) void window_join_kernel(WindowArgs A, FarPlan F, const float* __restrict__ part, T* __restrict__ dk,
+                                                              T* __restrict__ dv)
 {
-    __shared__ float s_sum[4][64];
-    const int keys = F.near_tiles * KEYS;
-    const int key = (int)(blockIdx.x % keys), hk = (int)(blockIdx.x / keys % A.Hkv), b = (int)(blockIdx.x / keys / A.Hkv);
+    __shared__ float s_sum[16][64];
+    const int keys = F.near_tiles * KEYS, sinks = min(A.sinks, keys), groups = sinks + (keys - sinks + 15) / 16;
+    const int g = (int)(blockIdx.x % groups), hk = (int)(blockIdx.x / groups % A.Hkv), b = (int)(blockIdx.x / groups / A.Hkv);
     const Sequence sq = sequence_of(A, b);
-    if (key >= sq.len) return;
-    const int G = A.Hq / A.Hkv, d = A.d, share = threadIdx.x >> 6, c0 = threadIdx.x & 63;
+    const int share = threadIdx.x >> 6, c0 = threadIdx.x & 63, G = A.Hq / A.Hkv, d = A.d;
+    const bool sink = g < sinks;
+    const int key = sink ? g : sinks + (g - sinks) * 16 + share;
+    const bool there = key < keys && key < sq.len;
+    if (sink && !there) return;
     const int start = far_start(key / KEYS, A.window);
     // far chunks that have rows: from the one that holds `start` on
-    const int c1 = start / F.chunk, n = key < A.sinks && start < sq.len ? (sq.len - 1) / F.chunk - c1 + 1 : 0;
+    const int c1 = start / F.chunk, n = sink && start < sq.len ? (sq.len - 1) / F.chunk - c1 + 1 : 0;
     const float* near = part + F.off_near / sizeof(float) + (((size_t)b * A.Hkv + hk) * F.near_tiles + key / KEYS) * 2 * KEYS * d;
     const float* far = part + F.off_far / sizeof(float) + ((((size_t)b * A.Hkv + hk) * F.blocks + key / FAR_KEYS) * G * F.chunks * 2 * FAR_KEYS +
                                                           key % FAR_KEYS) * d;
     const long long off = (long long)sq.tb * A.ks[0] + (long long)hk * A.ks[1] + (long long)(sq.first + key) * A.ks[2];
-    for (int i = 0; i < 2 * d; i += 64) {
-        const int which = i + c0 >= d, comp = which ? i + c0 - d : i + c0;
-        const bool there = i + c0 < 2 * d;
-        float sum = there && share == 0 ? near[((size_t)which * KEYS + key % KEYS) * d + comp] : 0.f;
+    for (int i = c0; i < round_up(2 * d, 64); i += 64) {
+        const int which = i >= d, comp = which ? i - d : i;
+        const bool mine = there && i < 2 * d;
+        float sum = mine && (!sink || share == 0) ? near[((size_t)which * KEYS + key % KEYS) * d + comp] : 0.f;
+        if (sink) {
+            if (mine) {
 #pragma unroll 4
-        for (int j = share * G * n / 4; there && j < (share + 1) * G * n / 4; ++j)
-            sum += far[((size_t)(j / n) * F.chunks + c1 + j % n) * 2 * FAR_KEYS * d + (size_t)which * FAR_KEYS * d + comp];
-        s_sum[share][c0] = sum;
-        __syncthreads();
-        if (share == 0 && there) {
-            sum = (s_sum[0][c0] + s_sum[1][c0]) + (s_sum[2][c0] + s_sum[3][c0]);
+                for (int j = share * G * n / 16; j < (share + 1) * G * n / 16; ++j)
+                    sum += far[((size_t)(j / n) * F.chunks + c1 + j % n) * 2 * FAR_KEYS * d + (size_t)which * FAR_KEYS * d + comp];
+            }
+            s_sum[share][c0] = sum;
+            __syncthreads();
+            sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum += s_sum[j][c0];
+            __syncthreads();
+        }
+        if (mine && (!sink || share == 0)) {
             const float y[8] = {sum, sum, sum, sum, sum, sum, sum, sum};
             const u32x4 p = Piece<T>::pack(y);
             __builtin_memcpy((which ? dv : dk) + off + comp, &p, sizeof(T));
         }
-        __syncthreads();
     }
 }
 
@@ -742,18 +658,19 @@ hipError_t launch_cap(const WindowArgs& A, const void* q_, const void* k_, const
     const int G = A.Hq / A.Hkv, blocks = (A.span_max + 31) / 32, ktiles = (A.span_max + KEYS - 1) / KEYS;
     const long long g1 = work_groups((long long)A.B * A.Hkv * ((blocks * G + 3) / 4)), g2 = work_groups((long long)A.B * A.Hkv * ktiles);
     const long long g3 = F.any ? work_groups((long long)A.B * A.Hkv * F.blocks * G * F.chunks) : 0;
-    const long long g4 = F.any ? (long long)A.B * A.Hkv * F.near_tiles * KEYS : 0;
+    const int near_keys = F.near_tiles * KEYS, sinks = std::min(A.sinks, near_keys);
+    const long long g4 = F.any ? (long long)A.B * A.Hkv * (sinks + (near_keys - sinks + 15) / 16) : 0;
     if (std::max(std::max(g1, g2), std::max(g3, g4)) > 0x7fffffffll) return hipErrorInvalidConfiguration;
     window_dq_kernel<T, D, CAP><<<(unsigned)g1, WTHR, 0, st>>>(A, blocks, q, k, v, out, lse, dout, delta, (T*)dq);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    window_dkv_kernel<T, D, CAP><<<(unsigned)g2, WTHR, 0, st>>>(A, F, ktiles, q, k, v, lse, dout, delta, part, dk, dv);
+    window_dkv_kernel<T, D, CAP><<<(unsigned)g2, dkv_threads<T, D>(), 0, st>>>(A, F, ktiles, q, k, v, lse, dout, delta, part, dk, dv);
     e = hipGetLastError();
     if (e != hipSuccess || !F.any) return e;
     window_far_kernel<T, D, CAP><<<(unsigned)g3, 64 * far_waves<T, D>(), 0, st>>>(A, F, q, k, v, lse, dout, delta, part);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    window_join_kernel<T><<<(unsigned)g4, WTHR, 0, st>>>(A, F, part, dk, dv);
+    window_join_kernel<T><<<(unsigned)g4, JOIN_THR, 0, st>>>(A, F, part, dk, dv);
     return hipGetLastError();
 }
 template <typename T, int D, typename... X>

@@ -235,26 +235,42 @@ __global__ __launch_bounds__(WTHR, (dec_waves<T, D>())) void window_step_kernel(
     }
 }
 
-// out and lse of a head from its work-groups' partial softmaxes
+// out and lse of a head from its work-groups' partial softmaxes (all of a thread's loads are on their way before the first is needed)
 template <typename T>
 __global__ __launch_bounds__(256) void window_step_join_kernel(WindowArgs A, int parts, const int* __restrict__ pos_dev,
                                                              const float* __restrict__ part, T* __restrict__ out, float* __restrict__ lse)
 {
+    constexpr int AT_ONCE = 16;
     const size_t bh = blockIdx.x;
-    if (!step_of(A, pos_dev[bh / A.Hq]).live) return;
-    const int d = A.d;
+    const int d = A.d, comp = threadIdx.x;
     const float* slots = part + bh * parts * (d + 2);
-    const int comp = threadIdx.x;
-    if (comp >= d) return;
-    float M = -INFINITY;
-    for (int i = 0; i < parts; ++i) M = fmaxf(M, slots[(size_t)i * (d + 2) + d]);
-    float l = 0.f, sum = 0.f;
-    for (int i = 0; i < parts; ++i) {
-        const float* s = slots + (size_t)i * (d + 2);
-        const float f = exp2f(s[d] - M);
-        l += s[d + 1] * f;
-        sum += s[comp] * f;
+    const int pos = pos_dev[bh / A.Hq];
+    float M = -1e30f, l = 0.f, sum = 0.f;
+    for (int i0 = 0; i0 < parts; i0 += AT_ONCE) {
+        float m[AT_ONCE], ls[AT_ONCE], o[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const bool there = i0 + i < parts;
+            const float* s = slots + (size_t)(there ? i0 + i : 0) * (d + 2);
+            m[i] = there ? s[d] : -1e30f;
+            ls[i] = there ? s[d + 1] : 0.f;
+            o[i] = there && comp < d ? s[comp] : 0.f;
+        }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) top = fmaxf(top, m[i]);
+        const float f = exp2f(M - top);
+        l *= f;
+        sum *= f;
+        M = top;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const float g = i0 + i < parts ? exp2f(m[i] - M) : 0.f;
+            l += ls[i] * g;
+            sum += o[i] * g;
+        }
     }
+    if (!step_of(A, pos).live || comp >= d) return;           // (what a skipped sequence's slots hold is not used)
     const float y = sum / l;
     const float ys[8] = {y, y, y, y, y, y, y, y};
     const u32x4 pk = Piece<T>::pack(ys);
