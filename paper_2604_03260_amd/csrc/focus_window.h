@@ -110,6 +110,20 @@ __device__ inline int opaque(int x)
     return x;
 }
 
+// The wait between a matrix product and the first read of its result by another instruction, in the source.  The compiler puts in what it has counted, but
+// where the read is a copy behind the end of a conditional part it has been seen to count along one of the two ways only, and a row's last
+// components came out wrong (5 of the 12 states that a 32x32x16 product needs).  So it is stated where results do not stay in their registers,
+// with long rows; there the loops' listings have the full count on all ways.
+template <typename T, int D>
+__device__ inline void settle()
+{
+    if constexpr (D * (int)sizeof(T) > 256) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 15\n\ts_nop 1");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // A tile of R rows of D components in LDS, the first operand of both kinds of product: by rows (its rows are the product's rows), and by components
 // (its components are; its rows are contracted, four at a time from the LDS reads that turn 4 x 16 values of 16 bits around, one by one for fp32).
 // Row r lies at r * RPITCH, its 16-byte piece c at place c ^ turn(r), so that neither kind of read meets a bank twice: the 16 consecutive rows
@@ -210,7 +224,7 @@ struct Dma {
 __device__ inline void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Values that are not finite, in a tile that some row does not see as a whole: the weight of what is hidden is zero, but 0 * inf is not.  They
-// become zeros, and their rows are marked (bit r of the two words at bad): whoever sees such a row is spoiled as a whole (spoiled_by).
+// become zeros, and their rows are marked (bit r of the words at bad): whoever sees such a row is spoiled as a whole (spoiled_by).
 // By all threads of the work-group, between two barriers.
 template <typename T, int D, int R>
 __device__ inline void scrub(char* tile, unsigned* bad)
@@ -325,42 +339,23 @@ __device__ inline void store_row(T* row, const f32x16* acc, float f, int lane)
         }
 }
 
-// The keys that rows first .. last can see, in blocks of 32 and tiles of U blocks: the sinks' blocks, then those from the first key of the
-// window on.  (A single block of sinks has a tile to itself, more of them whole tiles; the blocks behind the last sink are window like any.)
+// The keys that rows first .. last can see, in tiles of 32: the sinks', then those from the first key of the window on
 struct Walk {
-    int first, last, sink_blocks, sink_tiles, base, blocks, tiles;
+    int first, last, sink_tiles, base, tiles;
     int open0;                  // keys from here to the first row hide nothing
-    __device__ Walk(const WindowArgs& A, const Sequence& sq, int first_, int last_, int U)
+    __device__ Walk(const WindowArgs& A, int first_, int last_)
     {
         first = first_;
         last = last_;
-        sink_blocks = (min(A.sinks, last + 1) + 31) / 32;
-        if (sink_blocks > 1) sink_blocks = (sink_blocks + U - 1) / U * U;
-        sink_tiles = (sink_blocks + U - 1) / U;
-        base = max(32 * sink_blocks, max(0, first - A.window + 1) & ~31);
-        const int near = max(0, last / 32 - base / 32 + 1);
-        blocks = sink_blocks + near;
-        tiles = sink_tiles + (near + U - 1) / U;
+        sink_tiles = (min(A.sinks, last + 1) + 31) / 32;
+        base = max(32 * sink_tiles, max(0, first - A.window + 1) & ~31);
+        tiles = sink_tiles + max(0, last / 32 - base / 32 + 1);
         open0 = last - A.window + 1;
     }
-    __device__ int key_at(int t, int R) const { return t < sink_tiles ? t * R : base + (t - sink_tiles) * R; }
-    // may a pair of the rows and keys key0 .. key0 + R - 1 be hidden?
-    __device__ bool edge(int key0, int R, const WindowArgs& A) const
-    {
-        return key0 + R - 1 > first || (key0 < open0 && key0 + R - 1 >= A.sinks);
-    }
+    __device__ int key_at(int t) const { return t < sink_tiles ? 32 * t : base + 32 * (t - sink_tiles); }
+    // may a pair of the rows and keys key0 .. key0 + 31 be hidden?
+    __device__ bool edge(int key0, const WindowArgs& A) const { return key0 + 31 > first || (key0 < open0 && key0 + 31 >= A.sinks); }
 };
-// A block of a walk: tile and place in it
-struct At {
-    int t, u;
-};
-template <int U>
-__device__ inline At after(At a, const Walk& W)
-{
-    if (U == 1) return At{a.t + 1, 0};
-    const bool end = a.u == U - 1 || (a.t == 0 && W.sink_blocks == 1);
-    return At{end ? a.t + 1 : a.t, end ? 0 : a.u + 1};
-}
 
 // tanh of 16 scores times f: its series to z^9 while all are below 0.3 in magnitude (the next term is 1.6e-8 there, half a step of fp32
 // relative to z: six operations in place of an exponential and a reciprocal), else from exp(-2 |z|); fp32 takes the library's there.

@@ -5,11 +5,13 @@
 //         dQ^T += K^T dS^T); it also leaves delta for the next one
 //   dkv   a wavefront owns 32 keys and walks over the rows that see them, of every query head of the KV head in turn
 //         (S = Q K^T, dP = dout V^T, dV^T += dout^T P, dK^T += Q^T dS), so the sums over rows and heads have one order and need
-//         no atomics: seven products of a block instead of the five that a sum into dQ would take, and the same bits every time.
+//         no atomics: the same bits every time, for seven or eight products of a block (dkv_split) in place of the five that one walk would take.
 // The first `sinks` keys are seen by every row.  The rows behind their window are far too many for the wavefronts that own these keys:
 // work-groups of their own (far) take them in chunks, leave sums in 32 bits, and the last launch adds them to the owners' in order.
-// The products' operands are laid out as in the forward pass (focus_window.h): what is the A operand twice, by rows and by
-// components, is turned in registers on its way into LDS.
+// The products' operands lie in LDS as in the forward pass (focus_window.h): what is a first operand twice, by rows and by components, is copied
+// once and turned by the LDS reads.  The walk over the keys is the forward kernel's too: two buffers, one barrier per tile of 32, and the
+// wavefronts of a SIMD hide each other's waits (two at 128 components of 16 bits; 16384 tokens of 32/8 heads, window 1024: 515 us.  With one
+// that found its scores a block ahead and summed a block behind: 606).
 #include "focus_window.h"
 
 #include <algorithm>
@@ -20,10 +22,9 @@ using namespace window;
 
 namespace {
 
-// Keys of a dq tile: 32, so that two work-groups share a compute unit's LDS.  Rows of a dkv tile: what eight wavefronts fill evenly.
-constexpr int DQ_TILE = 32;
+// Rows of a dkv tile: what its wavefronts fill evenly.
 template <typename T, int D> constexpr int dkv_tile() { return D * (int)sizeof(T) > 512 || (sizeof(T) == 4 && (D == 64 || D == 128)) ? 32 : 64; }
-template <typename T, int D> constexpr int dq_waves() { return D * (int)sizeof(T) > 256 ? 1 : 2; }
+template <typename T, int D> constexpr int dq_waves() { return D * (int)sizeof(T) > 256 ? 1 : D * (int)sizeof(T) > 128 ? 2 : 3; }
 
 constexpr int KEYS = 128;                   // keys of a dkv work-group
 constexpr int FAR_KEYS = 32;                // ... of a far one, whose wavefronts share the rows
@@ -71,14 +72,11 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
                                                                            const T* __restrict__ dout, float* __restrict__ delta,
                                                                            T* __restrict__ dq)
 {
-    constexpr int R = DQ_TILE;
+    constexpr int R = 32;
     typedef Tile<T, D, R> TL;
     typedef Piece<T> P;
-    constexpr bool ROWS = D * (int)sizeof(T) <= 512;          // longer rows do not fit LDS often enough: by rows they are read from L1
-    constexpr int NK = ROWS ? 4 : 2;                          // K from a step before its scores to a step behind its dS
-    __shared__ __attribute__((aligned(256))) char s_k[NK][TL::BYTES];
-    __shared__ __attribute__((aligned(256))) char s_v[ROWS ? 2 : 1][ROWS ? TL::BYTES : 256];
-    __shared__ unsigned s_bad[4][2];
+    __shared__ __attribute__((aligned(256))) char s_k[2][TL::BYTES], s_v[2][TL::BYTES];
+    __shared__ unsigned s_bad[2];
     const int lane = threadIdx.x & 63, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int G = A.Hq / A.Hkv, fours = (blocks * G + 3) / 4;
@@ -90,6 +88,7 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
     if (tile0 >= sq.len) return;
     const int row0 = (four * 4 + wave) / G * 32;
     const int h = hk * G + (four * 4 + wave) % G;
+    const bool idle = row0 >= sq.len;
     const int row = row0 + (lane & 31);
     const bool real = row < sq.len;
     const int at = sq.first + (real ? row : sq.len - 1);
@@ -118,139 +117,76 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
     const float ci = CAP ? A.scale / A.softcap : 0.f;
 
     const int rplace = TL::rows_place(lane), cplace = TL::comps_place(lane);
-    // the forward kernel's walk with tiles of one block; step i: S and dP of block i + 1, dS of block i, dQ += dS K of block i - 1
-    const Walk W(A, sq, tile0, min((four * 4 + 3) / G * 32 + 32, sq.len) - 1, 1);
-    auto key_at = [&](int t) WINDOW_INLINE { return t < W.sink_tiles ? t * R : W.base + (t - W.sink_tiles) * R; };
+    const Walk W(A, tile0, min((four * 4 + 3) / G * 32 + 32, sq.len) - 1);
     const int pitch = (int)(A.ks[2] * (long long)sizeof(T));
     Dma<T, D, R, 4> dma;
     dma.init(wave, lane, pitch);
-    auto fetch = [&](const T* base, char* buf, int t) WINDOW_INLINE {
-        const int key = key_at(min(t, W.tiles - 1));
-        dma.load(base + (long long)key * A.ks[2], pitch, sq.len - key, buf, wave, lane);
+    auto fetch = [&](int t) WINDOW_INLINE {
+        const int key = W.key_at(t);
+        dma.load(kb + (long long)key * A.ks[2], pitch, sq.len - key, s_k[t & 1], wave, lane);
+        dma.load(vb + (long long)key * A.ks[2], pitch, sq.len - key, s_v[t & 1], wave, lane);
     };
-    auto fetch_both = [&](int t) WINDOW_INLINE {
-        fetch(kb, s_k[0] + (t & (NK - 1)) * TL::BYTES, t);
-        if constexpr (ROWS) fetch(vb, s_v[0] + (t & 1) * TL::BYTES, t);
-    };
-    // K of tile t has landed and is about to be met
-    auto check = [&](int t) WINDOW_INLINE {
-        if (threadIdx.x < 2) s_bad[(t + 1) & 3][threadIdx.x] = 0u;
-        if (t >= 0 && t < W.tiles && W.edge(key_at(t), R, A)) {
-            scrub<T, D, R>(s_k[0] + (t & (NK - 1)) * TL::BYTES, s_bad[t & 3]);
-            __syncthreads();
-        }
-    };
-    if (threadIdx.x < 8) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
-    for (int i = threadIdx.x; i < TL::BYTES / 16; i += WTHR) *(u32x4*)(s_k[NK - 1] + 16 * i) = u32x4{0u, 0u, 0u, 0u};
-    if constexpr (ROWS) {
-        fetch_both(0);
-        fetch_both(1);
-    }
-    dma_wait();
-    __syncthreads();
-    if constexpr (ROWS) check(0);
-
-    auto scores = [&](int t, f32x16& z, f32x16& dz) WINDOW_INLINE {
-        const int rp = opaque(rplace), r = min(key_at(t) + (lane & 31), sq.len - 1);
-        const char *kbuf = s_k[0] + (t & (NK - 1)) * TL::BYTES, *vbuf = s_v[0] + (ROWS ? (t & 1) * TL::BYTES : 0);
-        z = 0.f;
-        dz = 0.f;
-#pragma unroll
-        for (int s = 0; s < TL::KS; ++s) {
-            z = P::mma(ROWS ? TL::rows_piece(kbuf, rp, s) : load_piece(kb + (long long)r * A.ks[2], 2 * s + hh), qf[s], z);
-            dz = P::mma(ROWS ? TL::rows_piece(vbuf, rp, s) : load_piece(vb + (long long)r * A.ks[2], 2 * s + hh), gf[s], dz);
-        }
-    };
-    f32x16 x, dx;
-    u32x4 pf[TL::US];
-#pragma unroll
-    for (int s = 0; s < TL::US; ++s) pf[s] = 0u;
-    // soft-caps the scores and hides what a row does not see: exponents of -inf, and dP = delta, so that dS is zero whatever was there
-    const int open0 = row0 + 32 - A.window, open1 = row0 - 31;           // blocks from key open0 to open1 hide nothing
-    auto finish = [&](int key0) WINDOW_INLINE {
-        if (CAP) tanh_scores<T>(x, ci);
-        if (key0 >= open0 && key0 <= open1) return;
-        if (block_kind(row0, key0, A.window, A.sinks) == OPEN) return;
-        const int key = opaque(key0 + 4 * hh);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const bool seen = visible(row, key + 8 * (i / 4) + i % 4, A.window, A.sinks);
-            x[i] = seen ? x[i] : CAP ? -1e30f : -INFINITY;
-            dx[i] = seen ? dx[i] : 0.f;
-        }
-    };
-    auto look = [&](int t) WINDOW_INLINE {
-        const int key = key_at(t);
-        if (!W.edge(key, R, A)) return;
-        const unsigned marks = s_bad[t & 3][0];
-        if (marks != 0u && spoiled_by<true>(marks, row, key, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
-    };
-    constexpr bool AHEAD = ROWS && D * (int)sizeof(T) <= 256;           // (registers)
-    auto step = [&](int i) WINDOW_INLINE {
+    if (threadIdx.x < 2) s_bad[threadIdx.x] = 0u;
+    fetch(0);
+#pragma unroll 1
+    for (int t = 0; t < W.tiles; ++t) {
+        const int buf = t & 1, key0 = W.key_at(t);
         dma_wait();
         __syncthreads();
-        check(ROWS ? i + 1 : i - 1);
-        fetch_both(ROWS ? i + 2 : i);
-        const int cp = opaque(cplace), rp = opaque(rplace);
-        // (block -1 is the zeros)
-        const char* cbuf = s_k[0] + ((i - 1) & (NK - 1)) * TL::BYTES;
-        const char *kbuf = s_k[0] + ((i + 1) & (NK - 1)) * TL::BYTES, *vbuf = s_v[0] + (ROWS ? ((i + 1) & 1) * TL::BYTES : 0);
-        u32x4 ra[AHEAD ? 2 * TL::KS : 1];
-        if constexpr (AHEAD) {
+        const bool edge = W.edge(key0, A);
+        if (edge) {
+            scrub<T, D, R>(s_k[buf], &s_bad[buf]);
+            __syncthreads();
+        }
+        if (t + 1 < W.tiles) fetch(t + 1);
+        const Block kind = idle ? HIDDEN : block_kind(row0, key0, A.window, A.sinks);
+        if (kind != HIDDEN) {
+            const int rp = opaque(rplace), cp = opaque(cplace);
+            f32x16 x = 0.f, dx = 0.f;
 #pragma unroll
             for (int s = 0; s < TL::KS; ++s) {
-                ra[2 * s] = TL::rows_piece(kbuf, rp, s);
-                ra[2 * s + 1] = TL::rows_piece(vbuf, rp, s);
+                x = P::mma(TL::rows_piece(s_k[buf], rp, s), qf[s], x);
+                dx = P::mma(TL::rows_piece(s_v[buf], rp, s), gf[s], dx);
             }
-            __builtin_amdgcn_sched_barrier(0);
+            settle<T, D>();
+            if (CAP) tanh_scores<T>(x, ci);
+            if (kind == EDGE) {                               // hidden: an exponent of -inf, and dP = delta
+                const int key = opaque(key0 + 4 * hh);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool seen = visible(row, key + 8 * (i / 4) + i % 4, A.window, A.sinks);
+                    x[i] = seen ? x[i] : CAP ? -1e30f : -INFINITY;
+                    dx[i] = seen ? dx[i] : 0.f;
+                }
+            }
+            u32x4 pf[TL::US];
+#pragma unroll
+            for (int s = 0; s < TL::US; ++s) {
+                float ds[8];
+#pragma unroll
+                for (int j = 0; j < P::E; ++j) {
+                    const float z = x[s * P::E + j];
+                    ds[j] = __builtin_amdgcn_exp2f(fmaf(z, c, -lse2)) * (dx[s * P::E + j] - del);
+                    if (CAP) ds[j] = z > -2.f ? ds[j] * (1.f - z * z) : 0.f;
+                }
+                pf[s] = P::pack(ds);
+            }
+#pragma unroll
+            for (int s = 0; s < TL::US; ++s)
+#pragma unroll
+                for (int db = 0; db < TL::DB; ++db) acc[db] = P::mma(TL::comps_piece(s_k[buf], cp, db, s), pf[s], acc[db]);
+            settle<T, D>();
+            if (edge) {
+                const unsigned marks = s_bad[buf];
+                if (marks != 0u && spoiled_by<true>(marks, row, key0, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
+            }
         }
-        u32x4 pn[TL::US];
-#pragma unroll
-        for (int s = 0; s < TL::US; ++s) {
-            float ds[8];
-#pragma unroll
-            for (int j = 0; j < P::E; ++j) {
-                const float z = x[s * P::E + j];
-                ds[j] = __builtin_amdgcn_exp2f(fmaf(z, c, -lse2)) * (dx[s * P::E + j] - del);
-                if (CAP) ds[j] = z > -2.f ? ds[j] * (1.f - z * z) : 0.f;
-            }
-            pn[s] = P::pack(ds);
-            if constexpr (AHEAD) asm volatile("" : "+v"(pn[s]));
+        if (edge) {                                           // (the marks have been seen by all before they go)
+            __syncthreads();
+            if (threadIdx.x == 0) s_bad[buf] = 0u;
         }
-        if constexpr (AHEAD) {
-            __builtin_amdgcn_sched_barrier(0);
-            x = 0.f;
-            dx = 0.f;
-#pragma unroll
-            for (int s = 0; s < TL::KS; ++s) {
-                x = P::mma(ra[2 * s], qf[s], x);
-                dx = P::mma(ra[AHEAD ? 2 * s + 1 : 0], gf[s], dx);
-            }
-        } else scores(min(i + 1, W.tiles - 1), x, dx);
-#pragma unroll
-        for (int s = 0; s < TL::US; ++s)
-#pragma unroll
-            for (int db = 0; db < TL::DB; ++db) acc[db] = P::mma(TL::comps_piece(cbuf, cp, db, s), pf[s], acc[db]);
-#pragma unroll
-        for (int s = 0; s < TL::US; ++s) pf[s] = pn[s];
-        __builtin_amdgcn_sched_barrier(0);
-        finish(key_at(i + 1));
-        if (i > 0) look(i - 1);
-    };
-    scores(0, x, dx);
-    finish(key_at(0));
-#pragma unroll 1
-    for (int i = 0; i < W.blocks; ++i) step(i);
-    dma_wait();
-    __syncthreads();
-    const int i = W.blocks - 1;
-    if constexpr (!ROWS) check(i);
-    if (row0 >= sq.len) return;
-#pragma unroll
-    for (int s = 0; s < TL::US; ++s)
-#pragma unroll
-        for (int db = 0; db < TL::DB; ++db) acc[db] = P::mma(TL::comps_piece(s_k[0] + (i & (NK - 1)) * TL::BYTES, cplace, db, s), pf[s], acc[db]);
-    look(i);
+    }
+    if (idle) return;
     spoiled = halves_sum(spoiled);
     store_row<T, D>(real ? dq + qoff : nullptr, acc, A.scale + spoiled, lane);
 }
