@@ -110,18 +110,26 @@ __device__ inline int opaque(int x)
     return x;
 }
 
+// Operands loaded before a loop have arrived.  Otherwise the compiler waits for them at their use in the loop, every time around, and with them
+// for every load issued since: the copy of the next tile, which it does not count.
+template <int N>
+__device__ inline void landed(u32x4 (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
 // The wait between a matrix product and the first read of its result by another instruction, in the source.  The compiler puts in what it has counted, but
 // where the read is a copy behind the end of a conditional part it has been seen to count along one of the two ways only, and a row's last
-// components came out wrong (5 of the 12 states that a 32x32x16 product needs).  So it is stated where results do not stay in their registers,
-// with long rows; there the loops' listings have the full count on all ways.
-template <typename T, int D>
+// components came out wrong (5 of the 12 states that a 32x32x16 product needs; 18 for 32x32x2).  With it the listings
+// have the full count on all ways; it takes 1 to 3% of the time of a long 16-bit call.
+template <typename T>
 __device__ inline void settle()
 {
-    if constexpr (D * (int)sizeof(T) > 256) {
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_nop 15\n\ts_nop 1");
-        __builtin_amdgcn_sched_barrier(0);
-    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (sizeof(T) == 4) asm volatile("s_nop 15\n\ts_nop 1");
+    else asm volatile("s_nop 11");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // A tile of R rows of D components in LDS, the first operand of both kinds of product: by rows (its rows are the product's rows), and by components
@@ -217,7 +225,7 @@ struct Dma {
             for (int i = 0; i < N; ++i) lds_dma16(base, off[i], to + 1024 * i);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) lds_dma16(base, source(i, wave, lane, pitch, left), to + 1024 * i);
+            for (int i = 0; i < N; ++i) lds_dma16(base, source(i, wave, opaque(lane), pitch, left), to + 1024 * i);
         }
     }
 };
@@ -225,12 +233,12 @@ __device__ inline void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memor
 
 // Values that are not finite, in a tile that some row does not see as a whole: the weight of what is hidden is zero, but 0 * inf is not.  They
 // become zeros, and their rows are marked (bit r of the words at bad): whoever sees such a row is spoiled as a whole (spoiled_by).
-// By all threads of the work-group, between two barriers.
+// By `threads` threads, of which this is one: the work-group's between two barriers, or a wavefront's in a tile of its own.
 template <typename T, int D, int R>
-__device__ inline void scrub(char* tile, unsigned* bad)
+__device__ inline void scrub(char* tile, unsigned* bad, int thread, int threads)
 {
     typedef Tile<T, D, R> TL;
-    for (int id = threadIdx.x; id < TL::BYTES / 16; id += blockDim.x) {
+    for (int id = thread; id < TL::BYTES / 16; id += threads) {
         u32x4 v = *(const u32x4*)(tile + 16 * id);
         bool found = false;
 #pragma unroll

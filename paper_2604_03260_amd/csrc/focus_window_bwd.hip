@@ -10,7 +10,7 @@
 // work-groups of their own (far) take them in chunks, leave sums in 32 bits, and the last launch adds them to the owners' in order.
 // The products' operands lie in LDS as in the forward pass (focus_window.h): what is a first operand twice, by rows and by components, is copied
 // once and turned by the LDS reads.  The walk over the keys is the forward kernel's too: two buffers, one barrier per tile of 32, and the
-// wavefronts of a SIMD hide each other's waits (two at 128 components of 16 bits; 16384 tokens of 32/8 heads, window 1024: 515 us.  With one
+// wavefronts of a SIMD hide each other's waits (two at 128 components of 16 bits; 16384 tokens of 32/8 heads, window 1024: 520 us.  With one
 // that found its scores a block ahead and summed a block behind: 606).
 #include "focus_window.h"
 
@@ -128,6 +128,8 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
     };
     if (threadIdx.x < 2) s_bad[threadIdx.x] = 0u;
     fetch(0);
+    landed(qf);
+    landed(gf);
 #pragma unroll 1
     for (int t = 0; t < W.tiles; ++t) {
         const int buf = t & 1, key0 = W.key_at(t);
@@ -135,7 +137,7 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
         __syncthreads();
         const bool edge = W.edge(key0, A);
         if (edge) {
-            scrub<T, D, R>(s_k[buf], &s_bad[buf]);
+            scrub<T, D, R>(s_k[buf], &s_bad[buf], threadIdx.x, WTHR);
             __syncthreads();
         }
         if (t + 1 < W.tiles) fetch(t + 1);
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
                 x = P::mma(TL::rows_piece(s_k[buf], rp, s), qf[s], x);
                 dx = P::mma(TL::rows_piece(s_v[buf], rp, s), gf[s], dx);
             }
-            settle<T, D>();
+            settle<T>();
             if (CAP) tanh_scores<T>(x, ci);
             if (kind == EDGE) {                               // hidden: an exponent of -inf, and dP = delta
                 const int key = opaque(key0 + 4 * hh);
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(WTHR, (dq_waves<T, D>())) void window_dq_kernel(Win
             for (int s = 0; s < TL::US; ++s)
 #pragma unroll
                 for (int db = 0; db < TL::DB; ++db) acc[db] = P::mma(TL::comps_piece(s_k[buf], cp, db, s), pf[s], acc[db]);
-            settle<T, D>();
+            settle<T>();
             if (edge) {
                 const unsigned marks = s_bad[buf];
                 if (marks != 0u && spoiled_by<true>(marks, row, key0, hh, A.window, A.sinks)) spoiled = __builtin_nanf("");
@@ -338,6 +340,10 @@ __global__ __launch_bounds__((dkv_threads<T, D>()), 2) void window_dkv_kernel(Wi
     };
     if (threadIdx.x < 4) s_bad[threadIdx.x >> 1][threadIdx.x & 1] = 0u;
     fetch();
+    if constexpr (KEEP) {
+        landed(kf);
+        landed(vf);
+    }
     const int rplace = TL::rows_place(lane), cplace = TL::comps_place(lane);
 #pragma unroll 1
     for (int t = 0; t < ntiles; ++t) {
@@ -347,8 +353,8 @@ __global__ __launch_bounds__((dkv_threads<T, D>()), 2) void window_dkv_kernel(Wi
         __syncthreads();
         const bool edge = edge_row(row_t);
         if (edge) {
-            scrub<T, D, R>(s_q[buf], s_bad[buf]);
-            scrub<T, D, R>(s_g[buf], s_bad[buf]);
+            scrub<T, D, R>(s_q[buf], s_bad[buf], threadIdx.x, dkv_threads<T, D>());
+            scrub<T, D, R>(s_g[buf], s_bad[buf], threadIdx.x, dkv_threads<T, D>());
             __syncthreads();
         }
         advance(next);

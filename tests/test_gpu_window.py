@@ -268,3 +268,89 @@ def test_replay_from_a_graph_with_new_inputs():
         torch.cuda.synchronize()
         for x, y in zip(outs, run(p, *args)):
             assert torch.equal(x, y)
+
+
+# Calls with so many rows that a work-group has four pieces of 32 rows (the others share one piece; the choice goes by the number of
+# work-groups): the cases above are small.  Groups of 3 heads leave wavefronts of a work-group at different rows.
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d", [64, 80, 96, 128, 256])
+@pytest.mark.parametrize("cap", [0.0, 15.0])
+def test_forward_of_many_rows(d, dtype, cap):
+    B, Hq, Hkv, n, w, s = 8, 9, 3, 517, 65, 40
+    q, k, v = (rows(B, h, n, d, dtype, 80 + i) for i, h in enumerate((Hq, Hkv, Hkv)))
+    p = focus.make_window_params(B, Hq, Hkv, n, d, w, sinks=s, dtype=dtype, softcap=cap)
+    got = run(p, q, k, v)
+    for b in range(B):
+        ref = reference(q[b], k[b], v[b], w, s, 1 / math.sqrt(d), cap, dtype)
+        for name, x in zip(NAMES, got):
+            check(x[b], ref, name)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 128), ("f32", 64)])
+def test_spans_of_many_rows(dtype, d):
+    Hq, Hkv, w, s = 12, 4, 50, 3
+    lengths = [1, 333, 0, 64, 129, 2, 31, 600, 33, 128, 0, 7] * 3
+    gap, want, at = 3, [], 0
+    for x in lengths:
+        want.append((at, x))
+        at += x + gap
+    q, k, v = (rows(1, h, at, d, dtype, 90 + i) for i, h in enumerate((Hq, Hkv, Hkv)))
+    used = torch.zeros(at, dtype=torch.bool, device="cuda")
+    for first, length in want:
+        used[first:first + length] = True
+    for x in (q, k, v):
+        x[:, :, ~used] = float("nan")
+    p = focus.make_window_params(len(want), Hq, Hkv, at, d, w, sinks=s, dtype=dtype, packed=True, span_max=600)
+    got = run(p, q, k, v, spans=torch.tensor(want, dtype=torch.int32, device="cuda"), fill=7.0)
+    for name, x in zip(NAMES, got):
+        assert (x[:, :, ~used] == 7.0).all(), name
+    for first, length in want:
+        if length:
+            r = slice(first, first + length)
+            ref = reference(q[0, :, r], k[0, :, r], v[0, :, r], w, s, 1 / math.sqrt(d), 0.0, dtype)
+            for name, x in zip(NAMES, got):
+                check(x[0, :, r], ref, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_values_that_are_not_finite_among_many_rows(value, dtype):
+    B, Hq, Hkv, n, d, w, s = 48, 6, 3, 260, 64, 40, 3
+    q, k, v = (rows(B, h, n, d, dtype, 100 + i) for i, h in enumerate((Hq, Hkv, Hkv)))
+    p = focus.make_window_params(B, Hq, Hkv, n, d, w, sinks=s, dtype=dtype)
+    clean = run(p, q, k, v)
+    i = torch.arange(n, device="cuda")
+    apart = (i < 70) | (i >= 70 + w)
+    for where in ("k", "v"):
+        k2, v2 = k.clone(), v.clone()
+        (k2 if where == "k" else v2)[5, 1, 70, 5] = value
+        got = run(p, q, k2, v2)
+        sees = torch.zeros(B, Hq, n, dtype=torch.bool, device="cuda")
+        sees[5, 2:4] = ~apart
+        for j in (0, 1):
+            assert torch.equal(got[j][~sees], clean[j][~sees]), (where, NAMES[j])
+        if where == "k" and math.isinf(value):
+            sees &= q[..., 5] > 0
+        assert (~torch.isfinite(got[0].float()).all(-1))[sees].all()
+
+
+def test_short_calls_replayed_from_a_graph():
+    """A call of few rows in a graph, with new inputs and eager calls between the replays."""
+    B, H, n, d, w = 1, 8, 200, 64, 33
+    q, k, v = (rows(B, H, n, d, "bf16", 110 + i) for i in range(3))
+    p = focus.make_window_params(B, H, H, n, d, w, sinks=2)
+    out, lse = run(p, q, k, v)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            focus.focus_window_attn_fwd(p, q, k, v, out, lse)
+    torch.cuda.synchronize()
+    for i in range(4):
+        for j, x in enumerate((q, k, v)):
+            x.copy_(rows(B, H, n, d, "bf16", 120 + 3 * i + j))
+        graph.replay()
+        want = run(p, q, k, v)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
