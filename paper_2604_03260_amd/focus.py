@@ -3,7 +3,8 @@
 The functions mirror include/focus.h one to one (focus_workspace_size,
 focus_assign, focus_attn_fwd, focus_workspace_views, focus_route_workspace_size,
 focus_route, focus_assign_tokens, focus_attn_fwd_set, focus_attn_merge, focus_attn_fwd_two_call,
-focus_decode_state_size, focus_decode_prefill, focus_decode_step, focus_decode_state_views, focus_last_error, focus_version).  Tensors are torch CUDA tensors used purely as device buffers;
+focus_decode_state_size, focus_decode_prefill, focus_decode_step, focus_decode_state_views, focus_rope, focus_qk_norm_rope, focus_window_attn_fwd,
+focus_window_attn_bwd, focus_window_cache_fill, focus_window_decode_step_at and so on, focus_last_error, focus_version).  Tensors are torch CUDA tensors used purely as device buffers;
 the calls are enqueued on torch's current stream.  There is no CPU fallback: a
 missing library is an error.
 """
