@@ -221,12 +221,12 @@ def _check(st):
         raise FocusError(st, load_library().focus_last_error().decode())
 
 
-def _ptr(t):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
+def _ptr(t):                                           # (an int: every function has its argtypes)
+    return t.data_ptr() if t is not None else None
 
 
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return torch.cuda.current_stream().cuda_stream
 
 
 def focus_version():
