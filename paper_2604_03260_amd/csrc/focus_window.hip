@@ -24,7 +24,7 @@ namespace {
 
 constexpr int KEY_TILE = 32;
 // Wavefronts per SIMD: as many as the queries and the output leave registers for.  They are what hides the waits of a step whose parts depend on each
-// other (128 components of 16 bits, tiles of 32 keys: two 775 us, three 650 to 680 us; tiles of 64 keys, whose two buffers leave room for two
+// other (128 components of 16 bits, tiles of 32 keys: two 775 us, three 650 to 710 us by box; tiles of 64 keys, whose two buffers leave room for two
 // work-groups only, 785 us; 32768 tokens of 32/8 heads, window 1024).  Scores a block ahead of the softmax and operands a step ahead
 // of the products, with two wavefronts, were 769 us.
 template <typename T, int D> constexpr int fwd_waves() { return D * (int)sizeof(T) > 384 ? 1 : D * (int)sizeof(T) > 256 ? 2 : 3; }
